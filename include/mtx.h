@@ -344,6 +344,121 @@ int mtx_get_launches(const mtx_model* m, mtx_launch_info* out, int capacity, int
 /* Free the host handle (device buffers stay with the caller).  NULL is allowed. */
 void mtx_free_model(mtx_model* m);
 
+/* ---- token embedding, block norms, gradient clipping ----------------------------------------
+ * Operators on caller tensors, next to the layers MTX_EMBED and MTX_NORM and the clipped step
+ * (mtx_set_clip_norm), which run the same kernels.  Activations and tables are fp32 or bfloat16
+ * (an mtx_dtype names which), rows of D elements; `ld` arguments are strides between rows in
+ * elements; pointers are aligned to their element size at least (16-byte aligned rows are read
+ * faster).  Sums, statistics and parameter gradients are fp32 or wider.  Results are
+ * deterministic run to run: no sum depends on the order in which atomics arrive.  Every call may
+ * be captured into a HIP graph.  A workspace is 16-byte aligned device scratch whose content
+ * need not survive between calls: calls that overlap in time (other streams, other graphs) need
+ * workspaces of their own.  Operand tensors must not overlap unless stated. */
+
+/* Embedding lookup with scaling:  y[i][:] = scale * w[tokens[i]][:],  i < n, rounded once to
+ * y_type; w [V][D] contiguous of w_type, y rows ldy >= D apart.  A token equal to `pad` gives a
+ * row of zeros (pad < 0: no padding token); any other token outside [0, V) gives a row of NaN.
+ * n = 0 does nothing.  n < 2^31, V >= 1, D >= 1. */
+int mtx_embed_forward(const void* w, int w_type, int V, int D, const int32_t* tokens, size_t n,
+                      int pad, float scale, void* y, int y_type, size_t ldy, void* stream);
+
+/* Workspace of mtx_embed_backward for R shards of n tokens. */
+int mtx_embed_sizes(size_t n, int R, int V, int D, size_t* workspace_bytes);
+
+/* Gradient of the lookup, one per shard, in the shards' gradient rows:
+ *   grads[r*ld + t*D + d] = scale * sum over i < n with tokens[r*n + i] = t of dy[r*n + i][d]
+ * for every t < V (0 where no token is t), or with accumulate != 0 added to what is there (rows
+ * without a token are then neither read nor written).  Padding tokens and tokens outside [0, V)
+ * contribute nothing.  tokens [R*n]; dy [R*n] rows of dy_type, lddy >= D apart; ld >= V*D;
+ * R*n < 2^31.  The tokens are sorted, and each row's terms added in a fixed order. */
+int mtx_embed_backward(const int32_t* tokens, size_t n, int R, const void* dy, int dy_type,
+                       size_t lddy, int V, int D, int pad, float scale, float* grads, size_t ld,
+                       int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The end of one residual block and the norm before the next, in one pass over the rows:
+ *   u = norm(x; post_w, post_b)                  (u = x where post_w is NULL)
+ *   h_out = h + scale * gate * u                 (no gate where it is NULL; h_out = h where x is
+ *                                                 NULL: a norm alone)
+ *   y = norm(h_out; pre_w, pre_b)                (not computed where y is NULL)
+ * norm over the D elements of a row: MTX_NORM_RMS  t / sqrt(mean(t^2) + eps) * w  (the b are
+ * NULL), MTX_NORM_LAYER  (t - mean(t)) / sqrt(var(t) + eps) * w + b  (b may be NULL).  y is
+ * computed from h_out before it is rounded to `dtype`.
+ *   gate_rows = 0: one gate vector for all rows (a parameter: its gradient is per shard);
+ *   gate_rows > 0: gate [rows / gate_rows][D], one vector for each gate_rows rows in turn (a
+ *                  sequence's gate); must divide the rows of a shard.
+ * Weights and gates are fp32.  ld_h, ld_x, ld_y: strides between rows (0: D) of h and h_out (and
+ * dh, dh_out), of x (dx), of y (dy).  1 <= D <= 16384, rows < 2^31 (rows = 0 does nothing),
+ * eps >= 0. */
+typedef enum { MTX_NORM_RMS = 0, MTX_NORM_LAYER = 1 } mtx_norm_kind;
+typedef struct {
+    int kind;     /* mtx_norm_kind */
+    int dtype;    /* mtx_dtype of h, x, y and their gradients */
+    size_t rows;
+    int D;
+    float eps, scale;
+    size_t gate_rows;
+    const float *post_w, *post_b, *gate, *pre_w, *pre_b;
+    size_t ld_h, ld_x, ld_y;
+} mtx_norm_desc;
+
+/* stats (nullable) receives [rows][4] floats for the backward pass: mean and 1 / sqrt(var + eps)
+ * of x, then of h_out (mean 0 for MTX_NORM_RMS; the x pair is written only with post_w, the
+ * h_out pair only with y); 16-byte aligned.  h_out may be NULL, or h itself; where x is NULL it
+ * must be NULL. */
+int mtx_block_norm_forward(const mtx_norm_desc* d, const void* h, const void* x, void* h_out,
+                           void* y, float* stats, void* stream);
+
+/* Workspace of mtx_block_norm_backward for R shards of rows / R rows. */
+int mtx_block_norm_sizes(const mtx_norm_desc* d, int R, size_t* workspace_bytes);
+
+/* The backward pass.  h_out, x and stats are the forward pass's; dy (NULL: no gradient from y)
+ * and dh_out (NULL: none along the stream) the gradients of y and h_out, one at least.
+ *   dh [rows][D] (nullable): the gradient of h, dh_out + the gradient through y's norm;
+ *   dx [rows][D] (nullable): the gradient of x.
+ * dh may be dh_out itself.
+ *   d_post_w, d_post_b, d_pre_w, d_pre_b (each nullable): parameter gradients of shard r, the
+ *   sums over rows r*rows/R .. (r+1)*rows/R - 1, at [r*ld .. r*ld + D - 1] of each pointer;
+ *   d_gate (nullable): likewise for gate_rows = 0, else [rows / gate_rows][D] without stride.
+ * R must divide rows.  A gradient of an absent operand must be NULL. */
+int mtx_block_norm_backward(const mtx_norm_desc* d, int R, const void* h_out, const void* x,
+                            const float* stats, const void* dy, const void* dh_out, void* dh,
+                            void* dx, float* d_post_w, float* d_post_b, float* d_gate,
+                            float* d_pre_w, float* d_pre_b, size_t ld, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Global gradient norm and clipping.
+ *   norm = sqrt(sum g^2) over every element, summed in double;
+ *   factor = max_norm / norm where norm > max_norm, else 1;  clipped g = factor * g.
+ * max_norm > 0 (infinity: never clips).  A norm that is not finite clips nothing (factor 1):
+ * norm_out tells. */
+#define MTX_CLIP_WORKSPACE_BYTES 32768
+
+/* The average of R shard gradient rows (as mtx_average_grads), clipped: avg[i] = factor * (1/R)
+ * sum_r grads[r*ld + i], norm that of the average before clipping; norm_out (nullable, device
+ * fp32 [1]) receives it.  workspace: MTX_CLIP_WORKSPACE_BYTES. */
+int mtx_average_clip(const float* grads, int R, size_t n, size_t ld, float max_norm, float* avg,
+                     float* norm_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same over a list of tensors of either type.  Each is `n` contiguous elements at src (n may
+ * be 0); dst receives the clipped elements, rounded to dst_type: dst = src (same type) clips in
+ * place, dst = NULL only counts towards the norm.  No dst may overlap another tensor's src or
+ * dst.  The handle keeps the list in the caller's workspace (mtx_clip_sizes bytes, 256-byte
+ * aligned), which with the tensors must stay valid until mtx_free_clip; mtx_init_clip copies it
+ * there and synchronises with `stream`.  A handle must not be used on two streams at once. */
+typedef struct {
+    const void* src;
+    void* dst;
+    size_t n;
+    int src_type, dst_type;  /* mtx_dtype */
+} mtx_tensor;
+typedef struct mtx_clip mtx_clip;
+
+int mtx_clip_sizes(const mtx_tensor* tensors, int count, size_t* workspace_bytes);
+int mtx_init_clip(const mtx_tensor* tensors, int count, void* workspace, size_t workspace_bytes,
+                  void* stream, mtx_clip** out);
+int mtx_clip_grads(mtx_clip* c, float max_norm, float* norm_out, void* stream);
+void mtx_free_clip(mtx_clip* c);
+
 /* Message for the calling thread's last non-OK status ("" if none). */
 const char* mtx_last_error(void);
 

@@ -14,6 +14,7 @@
 #include <string>
 #include <vector>
 
+#include "api_common.h"
 #include "internal.h"
 
 using namespace mtx;
@@ -24,9 +25,10 @@ constexpr size_t kStaticScratchBytes = (size_t)64 << 20;
 static __device__ __align__(256) char scratch[kStaticScratchBytes];
 
 namespace {
-
 thread_local std::string g_err;
+}
 
+namespace mtx {
 int fail(int code, const char* fmt, ...)
 {
     char buf[512];
@@ -42,19 +44,13 @@ int hip_fail(hipError_t e, const char* what)
 {
     return fail(MTX_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
+}  // namespace mtx
 
-#define HIP_TRY(expr, what)                        \
-    do {                                           \
-        hipError_t _e = (expr);                    \
-        if (_e != hipSuccess) return hip_fail(_e, what); \
-    } while (0)
+namespace {
 
-constexpr size_t kAlign = 256;
 constexpr long long kMaxIndex = 2147483647LL;  // kernels index tensors with 32-bit ints
 constexpr long long kMaxBytes = 2147483647LL;  // and read them through 32-bit buffer offsets
 constexpr int kFarLimit = 8192;  // spatial sizes stay far below the kernels' out-of-window marker
-
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 struct LayerPlan {
     int kind, relu;
@@ -682,14 +678,6 @@ void glorot_init_host(const Plan& pl, uint64_t seed, std::vector<float>& w)
             w[lp.w_off + i] = (float)(a * (2.0 * u - 1.0));
         }
     }
-}
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-bool overlap(const void* a, size_t abytes, const void* b, size_t bbytes)
-{
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + bbytes && y < x + abytes;
 }
 
 }  // namespace

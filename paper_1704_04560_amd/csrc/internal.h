@@ -383,4 +383,61 @@ hipError_t conv_halo_wgrad_run(const ConvGeom& g, const RunGeom& rg, const HaloW
 hipError_t conv_halo_run(const ConvGeom& g, const RunGeom& r, const HaloPlan& h, const void* xp,
                          const void* w, const float* bias, bool relu, void* y, hipStream_t s);
 
+// embed.hip: rows of an embedding table by token, and its gradient (see mtx_embed_forward,
+// mtx_embed_backward).  R shards of n tokens each.
+hipError_t embed_fwd(const void* w, Dt wt, int V, int D, const int* tok, long long n, int pad,
+                     float scale, void* y, Dt yt, long long ldy, hipStream_t s);
+size_t embed_bwd_bytes(long long n, int R, int V, int D);
+hipError_t embed_bwd(const int* tok, long long n, int R, const void* dy, Dt dt, long long lddy,
+                     int V, int D, int pad, float scale, float* grads, long long ld,
+                     bool accumulate, void* ws, hipStream_t s);
+
+// blocknorm.hip: see mtx_block_norm_forward and mtx_block_norm_backward.  Strides are resolved
+// (not 0); group = rows of a gate vector (gate_rows, or the rows of a shard).
+constexpr int kNormMaxD = 16384;
+struct BlockNorm {
+    bool layer;
+    Dt dt;
+    long long rows;
+    int D;
+    float eps, scale;
+    long long gate_rows;
+    const float *post_w, *post_b, *gate, *pre_w, *pre_b;
+    long long ld_h, ld_x, ld_y;
+};
+hipError_t block_norm_fwd(const BlockNorm& b, const void* h, const void* x, void* h_out, void* y,
+                          float* stats, hipStream_t s);
+// Gradients wanted (each nullable) and their inputs.  relu_h: h_out is the output of a ReLU,
+// whose mask dh gets.
+struct BlockNormGrads {
+    const void *h_out, *x;
+    const float* stats;
+    const void *dy, *dh_out;
+    void *dh, *dx;
+    float *post_w, *post_b, *gate, *pre_w, *pre_b;
+    long long ld;
+    bool relu_h;
+};
+size_t block_norm_bwd_bytes(const BlockNorm& b, int R);
+hipError_t block_norm_bwd(const BlockNorm& b, int R, const BlockNormGrads& g, void* ws,
+                          hipStream_t s);
+
+// clip.hip: global gradient norm and clipping.  Partial sums of squares are doubles in scratch,
+// at most kClipBlocks of them.
+constexpr int kClipBlocks = 2048;
+// avg = (1/R) sum of the rows, clipped (in fp32 as average_update adds them, or exact: in double
+// as average_adapt does); norm_out, nonfinite (set to 0 or 1) nullable.
+hipError_t average_clip(const float* grads, int R, size_t n, size_t ld, bool exact, float max_norm,
+                        float* avg, float* norm_out, int* nonfinite, double* part, hipStream_t s);
+// One piece of a tensor of the list: n elements.
+struct ClipChunk {
+    const void* src;
+    void* dst;
+    unsigned n;
+    unsigned char src_bf16, dst_bf16, vec, pad;
+};
+constexpr size_t kClipChunk = 16384;
+hipError_t clip_list(const ClipChunk* chunks, int count, bool all_in_place, float max_norm,
+                     float* norm_out, double* part, hipStream_t s);
+
 }  // namespace mtx

@@ -20,6 +20,8 @@ MTX_OK, MTX_EINVAL, MTX_ENOMEM, MTX_EHIP, MTX_EUNSUPPORTED, MTX_ENONFINITE = 0, 
 MTX_F32, MTX_BF16 = 0, 1
 MTX_FC, MTX_CONV, MTX_MAXPOOL, MTX_BN, MTX_ADD, MTX_ADDP = 0, 1, 2, 3, 4, 5
 MTX_OPT_MOMENTUM, MTX_OPT_ADAM, MTX_OPT_ADAGRAD = 0, 1, 2
+MTX_NORM_RMS, MTX_NORM_LAYER = 0, 1
+MTX_CLIP_WORKSPACE_BYTES = 32768
 
 EXPORTS = ("mtx_model_sizes", "mtx_init_model", "mtx_init_model_static", "mtx_train_step", "mtx_average_grads",
            "mtx_sgd_update", "mtx_adam_update", "mtx_adagrad_update", "mtx_get_params",
@@ -27,7 +29,11 @@ EXPORTS = ("mtx_model_sizes", "mtx_init_model", "mtx_init_model_static", "mtx_tr
            "mtx_get_pool_argmax", "mtx_set_graph_replay", "mtx_set_overlap",
            "mtx_set_layerwise_update", "mtx_set_fused_update", "mtx_set_nonfinite_check",
            "mtx_set_timing",
-           "mtx_get_timing", "mtx_get_launches", "mtx_free_model", "mtx_last_error")
+           "mtx_get_timing", "mtx_get_launches", "mtx_free_model", "mtx_last_error",
+           "mtx_embed_forward", "mtx_embed_sizes", "mtx_embed_backward",
+           "mtx_block_norm_forward", "mtx_block_norm_sizes", "mtx_block_norm_backward",
+           "mtx_average_clip", "mtx_clip_sizes", "mtx_init_clip", "mtx_clip_grads",
+           "mtx_free_clip")
 
 
 class MtxError(RuntimeError):
@@ -70,6 +76,19 @@ class mtx_buffers(C.Structure):
                 ("workspace_bytes", C.c_size_t)]
 
 
+class mtx_norm_desc(C.Structure):
+    _fields_ = [("kind", C.c_int), ("dtype", C.c_int), ("rows", C.c_size_t), ("D", C.c_int),
+                ("eps", C.c_float), ("scale", C.c_float), ("gate_rows", C.c_size_t),
+                ("post_w", C.c_void_p), ("post_b", C.c_void_p), ("gate", C.c_void_p),
+                ("pre_w", C.c_void_p), ("pre_b", C.c_void_p),
+                ("ld_h", C.c_size_t), ("ld_x", C.c_size_t), ("ld_y", C.c_size_t)]
+
+
+class mtx_tensor(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("n", C.c_size_t),
+                ("src_type", C.c_int), ("dst_type", C.c_int)]
+
+
 _lib = None
 
 
@@ -108,6 +127,19 @@ def lib() -> C.CDLL:
             "mtx_get_launches": (i32, [vp, C.POINTER(mtx_launch_info), i32, C.POINTER(i32)]),
             "mtx_free_model": (None, [vp]),
             "mtx_last_error": (C.c_char_p, []),
+            "mtx_embed_forward": (i32, [vp, i32, i32, i32, vp, sz, i32, f32, vp, i32, sz, vp]),
+            "mtx_embed_sizes": (i32, [sz, i32, i32, i32, C.POINTER(sz)]),
+            "mtx_embed_backward": (i32, [vp, sz, i32, vp, i32, sz, i32, i32, i32, f32, vp, sz,
+                                         i32, vp, sz, vp]),
+            "mtx_block_norm_forward": (i32, [C.POINTER(mtx_norm_desc), vp, vp, vp, vp, vp, vp]),
+            "mtx_block_norm_sizes": (i32, [C.POINTER(mtx_norm_desc), i32, C.POINTER(sz)]),
+            "mtx_block_norm_backward": (i32, [C.POINTER(mtx_norm_desc), i32, *[vp] * 12, sz, vp,
+                                              sz, vp]),
+            "mtx_average_clip": (i32, [vp, i32, sz, sz, f32, vp, vp, vp, sz, vp]),
+            "mtx_clip_sizes": (i32, [C.POINTER(mtx_tensor), i32, C.POINTER(sz)]),
+            "mtx_init_clip": (i32, [C.POINTER(mtx_tensor), i32, vp, sz, vp, C.POINTER(vp)]),
+            "mtx_clip_grads": (i32, [vp, f32, vp, vp]),
+            "mtx_free_clip": (None, [vp]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -273,6 +305,130 @@ def mtx_get_launches(handle):
 
 def mtx_free_model(handle):
     lib().mtx_free_model(handle)
+
+
+def _bytes(t) -> int:
+    return 0 if t is None else t.nbytes
+
+
+def mtx_embed_forward(w, w_type, V, D, tokens, n, pad, scale, y, y_type, ldy, stream=None):
+    _check(lib().mtx_embed_forward(_ptr(w), w_type, V, D, _ptr(tokens), n, pad, scale, _ptr(y),
+                                   y_type, ldy, _stream(stream)))
+
+
+def mtx_embed_sizes(n, R, V, D) -> int:
+    out = C.c_size_t()
+    _check(lib().mtx_embed_sizes(n, R, V, D, C.byref(out)))
+    return out.value
+
+
+def mtx_embed_backward(tokens, n, R, dy, dy_type, lddy, V, D, pad, scale, grads, ld, accumulate,
+                       workspace, stream=None):
+    _check(lib().mtx_embed_backward(_ptr(tokens), n, R, _ptr(dy), dy_type, lddy, V, D, pad, scale,
+                                    _ptr(grads), ld, 1 if accumulate else 0, _ptr(workspace),
+                                    _bytes(workspace), _stream(stream)))
+
+
+def make_norm_desc(kind, dtype, rows, D, eps=1e-5, scale=1.0, gate_rows=0, post_w=None,
+                   post_b=None, gate=None, pre_w=None, pre_b=None, ld_h=0, ld_x=0, ld_y=0):
+    """mtx_norm_desc over the given weights, which it keeps alive."""
+    d = mtx_norm_desc(kind, dtype, rows, D, eps, scale, gate_rows, _ptr(post_w), _ptr(post_b),
+                      _ptr(gate), _ptr(pre_w), _ptr(pre_b), ld_h, ld_x, ld_y)
+    d._keep = (post_w, post_b, gate, pre_w, pre_b)
+    return d
+
+
+def mtx_block_norm_forward(desc, h, x, h_out, y, stats=None, stream=None):
+    _check(lib().mtx_block_norm_forward(C.byref(desc), _ptr(h), _ptr(x), _ptr(h_out), _ptr(y),
+                                        _ptr(stats), _stream(stream)))
+
+
+def mtx_block_norm_sizes(desc, R) -> int:
+    out = C.c_size_t()
+    _check(lib().mtx_block_norm_sizes(C.byref(desc), R, C.byref(out)))
+    return out.value
+
+
+def mtx_block_norm_backward(desc, R, h_out, x, stats, dy, dh_out, dh, dx, d_post_w, d_post_b,
+                            d_gate, d_pre_w, d_pre_b, ld, workspace, stream=None):
+    _check(lib().mtx_block_norm_backward(
+        C.byref(desc), R, _ptr(h_out), _ptr(x), _ptr(stats), _ptr(dy), _ptr(dh_out), _ptr(dh),
+        _ptr(dx), _ptr(d_post_w), _ptr(d_post_b), _ptr(d_gate), _ptr(d_pre_w), _ptr(d_pre_b), ld,
+        _ptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def mtx_average_clip(grads, R, n, ld, max_norm, avg, norm_out, workspace, stream=None):
+    _check(lib().mtx_average_clip(_ptr(grads), R, n, ld, max_norm, _ptr(avg), _ptr(norm_out),
+                                  _ptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def make_tensor_list(pairs):
+    """mtx_tensor array of (src, dst) torch tensors (contiguous, float32 or bfloat16; dst may be
+    None, or src itself)."""
+    import torch
+    types = {torch.float32: MTX_F32, torch.bfloat16: MTX_BF16}
+    arr = (mtx_tensor * len(pairs))()
+    for a, (src, dst) in zip(arr, pairs):
+        for t in (src, dst):
+            if t is None:
+                continue
+            if t.dtype not in types or not t.is_contiguous():
+                raise ValueError("tensors must be contiguous, float32 or bfloat16")
+            if t.numel() != src.numel() or t.device != src.device:
+                raise ValueError("src and dst must have the same length and device")
+        a.src, a.n, a.src_type = src.data_ptr(), src.numel(), types[src.dtype]
+        if dst is not None:
+            a.dst, a.dst_type = dst.data_ptr(), types[dst.dtype]
+    return arr
+
+
+def mtx_clip_sizes(tensors) -> int:
+    out = C.c_size_t()
+    _check(lib().mtx_clip_sizes(tensors, len(tensors), C.byref(out)))
+    return out.value
+
+
+def mtx_init_clip(tensors, workspace, stream=None):
+    handle = C.c_void_p()
+    _check(lib().mtx_init_clip(tensors, len(tensors), _ptr(workspace), _bytes(workspace),
+                               _stream(stream), C.byref(handle)))
+    return handle
+
+
+def mtx_clip_grads(handle, max_norm, norm_out=None, stream=None):
+    _check(lib().mtx_clip_grads(handle, max_norm, _ptr(norm_out), _stream(stream)))
+
+
+def mtx_free_clip(handle):
+    lib().mtx_free_clip(handle)
+
+
+class Clip:
+    """A list of (src, dst) tensors whose global norm is clipped (mtx_clip_grads), with its
+    workspace; keeps the tensors alive."""
+
+    def __init__(self, pairs, stream=None):
+        import torch
+        self.handle = None
+        self.pairs = list(pairs)
+        tensors = make_tensor_list(self.pairs)
+        self.workspace = torch.empty(mtx_clip_sizes(tensors), dtype=torch.uint8,
+                                     device=self.pairs[0][0].device)
+        self.handle = mtx_init_clip(tensors, self.workspace, stream)
+
+    def clip(self, max_norm, norm_out=None, stream=None):
+        mtx_clip_grads(self.handle, max_norm, norm_out, stream)
+
+    def close(self):
+        if self.handle:
+            mtx_free_clip(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 # ---- convenience wrapper owning the device buffers --------------------------------------------
