@@ -358,7 +358,7 @@ void mtx_free_model(mtx_model* m);
 /* Embedding lookup with scaling:  y[i][:] = scale * w[tokens[i]][:],  i < n, rounded once to
  * y_type; w [V][D] contiguous of w_type, y rows ldy >= D apart.  A token equal to `pad` gives a
  * row of zeros (pad < 0: no padding token); any other token outside [0, V) gives a row of NaN.
- * n = 0 does nothing.  n < 2^31, V >= 1, D >= 1. */
+ * n = 0 does nothing.  V, D >= 1, V <= 2^28, n <= 2^30, n*D <= 2^36. */
 int mtx_embed_forward(const void* w, int w_type, int V, int D, const int32_t* tokens, size_t n,
                       int pad, float scale, void* y, int y_type, size_t ldy, void* stream);
 
@@ -369,8 +369,9 @@ int mtx_embed_sizes(size_t n, int R, int V, int D, size_t* workspace_bytes);
  *   grads[r*ld + t*D + d] = scale * sum over i < n with tokens[r*n + i] = t of dy[r*n + i][d]
  * for every t < V (0 where no token is t), or with accumulate != 0 added to what is there (rows
  * without a token are then neither read nor written).  Padding tokens and tokens outside [0, V)
- * contribute nothing.  tokens [R*n]; dy [R*n] rows of dy_type, lddy >= D apart; ld >= V*D;
- * R*n < 2^31.  The tokens are sorted, and each row's terms added in a fixed order. */
+ * contribute nothing (their rows of dy are not read).  tokens [R*n]; dy [R*n] rows of dy_type,
+ * lddy >= D apart; ld >= V*D; R <= 65536, R*V <= 2^28, R*n <= 2^30, R*n*D <= 2^36.  The tokens are
+ * sorted, and each row's terms added in a fixed order. */
 int mtx_embed_backward(const int32_t* tokens, size_t n, int R, const void* dy, int dy_type,
                        size_t lddy, int V, int D, int pad, float scale, float* grads, size_t ld,
                        int accumulate, void* workspace, size_t workspace_bytes, void* stream);

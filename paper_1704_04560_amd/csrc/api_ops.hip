@@ -43,13 +43,16 @@ bool spans_overlap(std::initializer_list<Span> list)
 }
 
 constexpr size_t kMaxRows = 2147483647;
+constexpr size_t kMaxTokens = (size_t)1 << 30;
 
 int check_embed(int V, int D, size_t n, int R)
 {
     if (V < 1 || D < 1) return fail(MTX_EINVAL, "V and D must be >= 1 (got %d, %d)", V, D);
-    if (R < 1) return fail(MTX_EINVAL, "R must be >= 1 (got %d)", R);
-    if (n > kMaxRows || n * (size_t)R > kMaxRows)
-        return fail(MTX_EINVAL, "more than 2^31 - 1 tokens");
+    if (R < 1 || R > 65536) return fail(MTX_EINVAL, "R must lie in 1 .. 65536 (got %d)", R);
+    if (n > kMaxTokens || n * (size_t)R > kMaxTokens)
+        return fail(MTX_EINVAL, "more than 2^30 tokens");
+    if ((size_t)V * R > ((size_t)1 << 28)) return fail(MTX_EINVAL, "more than 2^28 table rows");
+    if (n * (size_t)R * D > ((size_t)1 << 36)) return fail(MTX_EINVAL, "more than 2^36 elements");
     return MTX_OK;
 }
 
