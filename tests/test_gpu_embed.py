@@ -65,6 +65,9 @@ CASES = [  # V, D, n, R, pad, scale, token law, extra lddy, offset, extra ld
     (65, 130, 4097, 2, 7, 2.0, "one", 0, 0, 2), (20000, 8, 3000, 1, -1, 1.0, "uniform", 0, 0, 0),
     (70001, 4, 5000, 3, -1, 1.0, "zipf", 0, 0, 5), (17, 5000, 300, 1, 16, 1.0, "zipf", 0, 0, 0),
     (3, 1, 9000, 1, 2, 1.0, "uniform", 0, 0, 0), (600, 256, 128, 8, -1, 1.0, "two", 0, 0, 0),
+    (500, 200, 3001, 2, 0, 1.0, "zipf", 0, 0, 4), (300, 1032, 2500, 1, -1, 0.5, "zipf", 8, 0, 0),
+    (900, 264, 1025, 3, -1, 1.0, "uniform", 0, 0, 0), (50, 16, 70000, 1, -1, 1.0, "one", 0, 0, 0),
+    (30, 128, 6000, 2, 29, 1.0, "two", 0, 0, 0), (40, 2056, 1024, 1, -1, 1.0, "one", 0, 0, 0),
 ]
 
 
