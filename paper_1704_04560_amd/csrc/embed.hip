@@ -25,17 +25,85 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const TW* __restrict__ w
     }
 }
 
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// 8 values as one or two 16-byte vectors.
+template <typename T> __device__ __forceinline__ void load8(const T* p, float (&v)[8])
+{
+#pragma unroll
+    for (int k = 0; k < 8; k += 16 / (int)sizeof(T)) {
+        const u32x4 raw = *reinterpret_cast<const u32x4*>(p + k);
+        const T* e = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+        for (int j = 0; j < 16 / (int)sizeof(T); ++j) v[k + j] = to_f32<T>(e[j]);
+    }
+}
+
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&v)[8])
+{
+#pragma unroll
+    for (int k = 0; k < 8; k += 16 / (int)sizeof(T)) {
+        u32x4 raw;
+        T* e = reinterpret_cast<T*>(&raw);
+#pragma unroll
+        for (int j = 0; j < 16 / (int)sizeof(T); ++j) e[j] = from_f32<T>(v[k + j]);
+        *reinterpret_cast<u32x4*>(p + k) = raw;
+    }
+}
+
+// D a multiple of 8 and 16-byte aligned rows: a thread takes 8 values at a time, rpb rows to a block
+// of 256 (one from D = 2048 on).  Bound by HBM, less what repeated tokens find in the caches:
+// 32768 tokens x 4096 from fp32 rows to bf16 97 us (8.3 TB/s of rows read and written; one value per
+// thread and access 199 us).
+template <typename TW, typename TY>
+__global__ __launch_bounds__(256) void embed_fwd_vec_kernel(const TW* __restrict__ w, int V, int D,
+                                                            const int* __restrict__ tok,
+                                                            long long n, int pad, float scale,
+                                                            TY* __restrict__ y, long long ldy,
+                                                            int rpb)
+{
+    const int units = D / 8, rr = threadIdx.x / units;
+    const int u0 = rpb > 1 ? threadIdx.x - rr * units : threadIdx.x;
+    if (rpb > 1 && rr >= rpb) return;
+    for (long long i = (long long)blockIdx.x * rpb + (rpb > 1 ? rr : 0); i < n;
+         i += (long long)gridDim.x * rpb) {
+        const int t = tok[i];
+        const bool in = (unsigned)t < (unsigned)V;
+        const bool zero = pad >= 0 && t == pad;
+        const TW* row = w + (long long)(in ? t : 0) * D;
+        const float f = in ? scale : __builtin_nanf("");
+        TY* out = y + i * ldy;
+#pragma unroll 2
+        for (int u = u0; u < units; u += 256) {
+            float v[8];
+            load8<TW>(row + 8 * u, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = zero ? 0.f : f * v[k];   // (the row may hold inf)
+            store8<TY>(out + 8 * u, v);
+        }
+    }
+}
+
 hipError_t embed_fwd(const void* w, Dt wt, int V, int D, const int* tok, long long n, int pad,
                      float scale, void* y, Dt yt, long long ldy, hipStream_t s)
 {
     if (n == 0) return hipSuccess;
-    const dim3 grid((unsigned)std::min<long long>(n, 65536));
+    auto al = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
+    const bool vec = D % 8 == 0 && ldy % 8 == 0 && al(w) && al(y);
+    const int rpb = std::max(1, 256 / std::max(1, D / 8));
     auto go = [&](auto tw, auto ty) {
         using TW = decltype(tw);
         using TY = decltype(ty);
-        hipLaunchKernelGGL((embed_fwd_kernel<TW, TY>), grid, dim3(256), 0, s,
-                           static_cast<const TW*>(w), V, D, tok, n, pad, scale,
-                           static_cast<TY*>(y), ldy);
+        if (vec)
+            hipLaunchKernelGGL((embed_fwd_vec_kernel<TW, TY>),
+                               dim3((unsigned)std::min<long long>((n + rpb - 1) / rpb, 1 << 22)),
+                               dim3(256), 0, s, static_cast<const TW*>(w), V, D, tok, n, pad, scale,
+                               static_cast<TY*>(y), ldy, rpb);
+        else
+            hipLaunchKernelGGL((embed_fwd_kernel<TW, TY>),
+                               dim3((unsigned)std::min<long long>(n, 65536)), dim3(256), 0, s,
+                               static_cast<const TW*>(w), V, D, tok, n, pad, scale,
+                               static_cast<TY*>(y), ldy);
     };
     if (wt == DT_F32) yt == DT_F32 ? go(float(), float()) : go(float(), bf16_t());
     else yt == DT_F32 ? go(bf16_t(), float()) : go(bf16_t(), bf16_t());
@@ -254,7 +322,6 @@ __device__ __forceinline__ void load_row(const T* p, int c, int D, float (&v)[E]
         constexpr int W = 16 / sizeof(T);
 #pragma unroll
         for (int k = 0; k < E; k += W) {
-            typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
             const u32x4 raw = *reinterpret_cast<const u32x4*>(p + c + k);
             const T* e = reinterpret_cast<const T*>(&raw);
 #pragma unroll
