@@ -7,82 +7,91 @@
 //   d_gate = scale sum dH u.
 // Statistics and sums are fp32; only h_out, y, dh and dx are rounded to the tensors' type.
 //
-// A row is held in the registers of NT threads, 8 C elements each, so that every tensor is read
-// and written once: both passes are bound by HBM.  Rows of at most 512 elements take one wave and
-// need no barrier.  Elements come in 16-byte vectors where D and the strides are multiples of
-// 8 and the pointers aligned (VEC), else singly, NT apart.
+// A row is held in the registers of NT threads, C times 16 bytes each, so that every tensor is read
+// and written once: both passes are bound by HBM.  Rows of at most 1 KB take one wave and need no
+// barrier.
 #include "device_common.h"
 #include "internal.h"
 
 #include <algorithm>
 #include <initializer_list>
+#include <type_traits>
 
 namespace mtx {
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-// Where a thread's element k of 8 C lies in the row.
-template <int NT, bool VEC> __device__ __forceinline__ int elem(int l, int k)
+// A thread's N = W C elements.  AL (rows of a multiple of W elements, aligned): runs of W, element k at
+// ((k / W) NT + l) W + k % W, so that a wave's vector loads are contiguous.  Else singly, element
+// k at k NT + l (unaligned vectors were slower: 8850 rows of 771 fp32, backward, 65 -> 89 us).
+template <int NT, int W, bool AL> __device__ __forceinline__ int elem(int l, int k)
 {
-    return VEC ? ((k / 8) * NT + l) * 8 + k % 8 : k * NT + l;
+    return AL ? ((k / W) * NT + l) * W + k % W : k * NT + l;
 }
 
-// A thread's elements of a row as they are stored.
-template <typename T, int N, bool VEC> struct Raw {
-    static constexpr int kVecs = N * (int)sizeof(T) / 16;
-    u32x4 v[VEC ? kVecs : 1];
-    T e[VEC ? 1 : N];
+template <int BYTES> struct Vec { typedef u32x4 type; };
+template <> struct Vec<8> { typedef unsigned type __attribute__((ext_vector_type(2))); };
+
+// N elements as they are stored: 32-bit words (AL), or one by one.
+template <typename T, int N, bool AL> struct Raw {
+    unsigned w[AL ? N * (int)sizeof(T) / 4 : 1];
+    T e[AL ? 1 : N];
 };
 
-template <typename T, int NT, int C, bool VEC>
-__device__ __forceinline__ void load_raw(const T* p, int l, int D, Raw<T, 8 * C, VEC>& o)
+template <typename T, int NT, int W, int C, bool AL>
+__device__ __forceinline__ void load_raw(const T* p, int l, int D, Raw<T, W * C, AL>& o)
 {
-    if constexpr (VEC) {
-        constexpr int per = (int)sizeof(T) / 2;   // vectors to 8 elements
+    if constexpr (AL) {
+        typedef typename Vec<W * (int)sizeof(T)>::type V;
+        constexpr int words = sizeof(V) / 4, per = W * (int)sizeof(T) / (int)sizeof(V);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int d = (c * NT + l) * 8;
+            const int d = (c * NT + l) * W;
 #pragma unroll
-            for (int q = 0; q < per; ++q)
-                o.v[c * per + q] = d < D ? reinterpret_cast<const u32x4*>(p + d)[q]
-                                         : u32x4{0u, 0u, 0u, 0u};
+            for (int q = 0; q < per; ++q) {
+                V v{};
+                if (d < D) v = reinterpret_cast<const V*>(p + d)[q];
+#pragma unroll
+                for (int j = 0; j < words; ++j) o.w[(c * per + q) * words + j] = v[j];
+            }
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < 8 * C; ++k) o.e[k] = k * NT + l < D ? p[k * NT + l] : T(0);
+        for (int k = 0; k < W * C; ++k) o.e[k] = k * NT + l < D ? p[k * NT + l] : T(0);
     }
 }
 
-template <typename T, int N, bool VEC>
-__device__ __forceinline__ float raw_at(const Raw<T, N, VEC>& o, int k)
+template <typename T, int N, bool AL>
+__device__ __forceinline__ float raw_at(const Raw<T, N, AL>& o, int k)
 {
-    if constexpr (VEC) {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(o.v[k / 4][k % 4]);
-        const unsigned u = o.v[k / 8][(k % 8) / 2];
-        return __uint_as_float(k % 2 ? u & 0xffff0000u : u << 16);
-    } else {
-        return to_f32<T>(o.e[k]);
-    }
+    if constexpr (!AL) return to_f32<T>(o.e[k]);
+    else if constexpr (sizeof(T) == 4) return __uint_as_float(o.w[k]);
+    else return __uint_as_float(k % 2 ? o.w[k / 2] & 0xffff0000u : o.w[k / 2] << 16);
 }
 
-template <typename T, int NT, int C, bool VEC>
-__device__ __forceinline__ void store_row(T* p, int l, int D, const float (&v)[8 * C])
+template <typename T, int NT, int W, int C, bool AL>
+__device__ __forceinline__ void store_row(T* p, int l, int D, const float (&v)[W * C])
 {
-    if constexpr (VEC) {
-        constexpr int W = 16 / (int)sizeof(T);
+    if constexpr (AL) {
+        typedef typename Vec<W * (int)sizeof(T)>::type V;
+        constexpr int per = W * (int)sizeof(T) / (int)sizeof(V);
 #pragma unroll
-        for (int k = 0; k < 8 * C; k += W) {
-            const int d = elem<NT, true>(l, k);
+        for (int c = 0; c < C; ++c) {
+            const int d = (c * NT + l) * W;
             if (d >= D) continue;
-            u32x4 raw;
-            T* e = reinterpret_cast<T*>(&raw);
+            T e[W];
 #pragma unroll
-            for (int j = 0; j < W; ++j) e[j] = from_f32<T>(v[k + j]);
-            *reinterpret_cast<u32x4*>(p + d) = raw;
+            for (int k = 0; k < W; ++k) e[k] = from_f32<T>(v[W * c + k]);
+#pragma unroll
+            for (int q = 0; q < per; ++q) {
+                V raw;
+                __builtin_memcpy(&raw, e + q * W / per, sizeof(V));
+                reinterpret_cast<V*>(p + d)[q] = raw;
+            }
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < 8 * C; ++k)
+        for (int k = 0; k < W * C; ++k)
             if (k * NT + l < D) p[k * NT + l] = from_f32<T>(v[k]);
     }
 }
@@ -90,7 +99,7 @@ __device__ __forceinline__ void store_row(T* p, int l, int D, const float (&v)[8
 // Sums over the NT threads of a row, the same bits in each.  `slot` alternates between calls: a
 // wave writes the slot of two calls ago only after a barrier that follows all its reads.
 template <int NT, int M>
-__device__ __forceinline__ void row_sum(float (&v)[M], float (&red)[2][M > 1 ? 2 : 1][16], int& slot)
+__device__ __forceinline__ void row_sum(float (&v)[M], float (&red)[2][M][16], int& slot)
 {
 #pragma unroll
     for (int m = 0; m < M; ++m)
@@ -114,11 +123,11 @@ __device__ __forceinline__ void row_sum(float (&v)[M], float (&red)[2][M > 1 ? 2
 
 constexpr int block_of(int NT) { return NT < 256 ? 256 : NT; }
 
-template <typename T, int NT, int C, bool VEC, bool LAYER>
+template <typename T, int W, int NT, int C, bool AL, bool LAYER>
 __global__ __launch_bounds__(block_of(NT)) void norm_fwd_kernel(BlockNorm b, const T* h, const T* x,
                                                                 T* h_out, T* y, float* stats)
 {
-    constexpr int N = 8 * C, RPB = block_of(NT) / NT;
+    constexpr int N = W * C, RPB = block_of(NT) / NT;
     __shared__ float red[2][1][16];
     int slot = 0;
     const int l = threadIdx.x % NT, D = b.D;
@@ -127,9 +136,9 @@ __global__ __launch_bounds__(block_of(NT)) void norm_fwd_kernel(BlockNorm b, con
     const long long want = (long long)blockIdx.x * RPB + threadIdx.x / NT;
     const bool live = want < b.rows;
     const long long i = live ? want : b.rows - 1;
-    Raw<T, N, VEC> rh, rx;
-    load_raw<T, NT, C, VEC>(h + i * b.ld_h, l, D, rh);
-    if (x) load_raw<T, NT, C, VEC>(x + i * b.ld_x, l, D, rx);
+    Raw<T, N, AL> rh, rx;
+    load_raw<T, NT, W, C, AL>(h + i * b.ld_h, l, D, rh);
+    if (x) load_raw<T, NT, W, C, AL>(x + i * b.ld_x, l, D, rx);
     auto norm = [&](float (&v)[N], const float* w, const float* bias, int stat) {
         float s[1], mean = 0.f;
         if constexpr (LAYER) {
@@ -142,16 +151,16 @@ __global__ __launch_bounds__(block_of(NT)) void norm_fwd_kernel(BlockNorm b, con
         s[0] = 0.f;
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const float t = LAYER && elem<NT, VEC>(l, k) >= D ? 0.f : v[k] - mean;
+            const float t = LAYER && elem<NT, W, AL>(l, k) >= D ? 0.f : v[k] - mean;
             s[0] = fmaf(t, t, s[0]);
         }
         row_sum<NT, 1>(s, red, slot);
         const float r = 1.0f / sqrtf(s[0] * inv_d + b.eps);
         if (stats && live && l == 0)
             *reinterpret_cast<float2*>(stats + 4 * i + stat) = make_float2(mean, r);
-        Raw<float, N, VEC> rw, rb;
-        load_raw<float, NT, C, VEC>(w, l, D, rw);
-        if (LAYER && bias) load_raw<float, NT, C, VEC>(bias, l, D, rb);
+        Raw<float, N, AL> rw, rb;
+        load_raw<float, NT, W, C, AL>(w, l, D, rw);
+        if (LAYER && bias) load_raw<float, NT, W, C, AL>(bias, l, D, rb);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             v[k] = (v[k] - mean) * r * raw_at(rw, k);
@@ -167,65 +176,79 @@ __global__ __launch_bounds__(block_of(NT)) void norm_fwd_kernel(BlockNorm b, con
         for (int k = 0; k < N; ++k) u[k] = raw_at(rx, k);
         if (b.post_w) norm(u, b.post_w, b.post_b, 0);
         if (b.gate) {
-            Raw<float, N, VEC> rg;
-            load_raw<float, NT, C, VEC>(b.gate + (b.gate_rows ? i / b.gate_rows : 0) * D, l, D, rg);
+            Raw<float, N, AL> rg;
+            load_raw<float, NT, W, C, AL>(b.gate + (b.gate_rows ? i / b.gate_rows : 0) * D, l, D, rg);
 #pragma unroll
             for (int k = 0; k < N; ++k) H[k] = fmaf(b.scale * raw_at(rg, k), u[k], H[k]);
         } else {
 #pragma unroll
             for (int k = 0; k < N; ++k) H[k] = fmaf(b.scale, u[k], H[k]);
         }
-        if (h_out && live) store_row<T, NT, C, VEC>(h_out + i * b.ld_h, l, D, H);
+        if (h_out && live) store_row<T, NT, W, C, AL>(h_out + i * b.ld_h, l, D, H);
     }
     if (!y) return;
     norm(H, b.pre_w, b.pre_b, 2);
-    if (live) store_row<T, NT, C, VEC>(y + i * b.ld_y, l, D, H);
+    if (live) store_row<T, NT, W, C, AL>(y + i * b.ld_y, l, D, H);
 }
 
 static bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+// Elements of a run: 16 bytes, or 8 of bf16 where a backward thread with 8 would not fit the 128
+// registers of two blocks to a compute unit (the biases' sums of a layer norm, single elements).
+template <typename T, bool LAYER, bool AL>
+constexpr int kRun = sizeof(T) == 4 || LAYER || !AL ? 4 : 8;
+
+// Calls go(type, layer norm, aligned) as constants.
+template <class F> static void with_form(const BlockNorm& b, bool al, F go)
+{
+    auto by_type = [&](auto t) {
+        if (b.layer) al ? go(t, std::true_type(), std::true_type()) : go(t, std::true_type(), std::false_type());
+        else al ? go(t, std::false_type(), std::true_type()) : go(t, std::false_type(), std::false_type());
+    };
+    if (b.dt == DT_F32) by_type(float());
+    else by_type(bf16_t());
+}
+
 static bool norm_vec(const BlockNorm& b, std::initializer_list<const void*> ptrs)
 {
-    bool ok = b.D % 8 == 0 && b.ld_h % 8 == 0 && b.ld_x % 8 == 0 && b.ld_y % 8 == 0 &&
+    const int w = b.dt == DT_F32 ? 4 : 8;
+    bool ok = b.D % w == 0 && b.ld_h % w == 0 && b.ld_x % w == 0 && b.ld_y % w == 0 &&
               al16(b.post_w) && al16(b.post_b) && al16(b.gate) && al16(b.pre_w) && al16(b.pre_b);
     for (const void* p : ptrs) ok = ok && al16(p);
     return ok;
 }
 
-template <typename T, int NT, int C>
-static void launch_fwd(const BlockNorm& b, bool vec, const void* h, const void* x, void* h_out,
-                       void* y, float* stats, hipStream_t s)
+// Calls f(NT, C) as constants: the threads of a row of W elements a thread and step.
+template <int W, class F> static void with_row_shape(int D, F f)
 {
-    constexpr int RPB = block_of(NT) / NT;
-    const dim3 grid((unsigned)((b.rows + RPB - 1) / RPB)), block(block_of(NT));
-    const T *hh = static_cast<const T*>(h), *xx = static_cast<const T*>(x);
-    T *ho = static_cast<T*>(h_out), *yy = static_cast<T*>(y);
-    if (vec && b.layer)
-        hipLaunchKernelGGL((norm_fwd_kernel<T, NT, C, true, true>), grid, block, 0, s, b, hh, xx, ho, yy, stats);
-    else if (vec)
-        hipLaunchKernelGGL((norm_fwd_kernel<T, NT, C, true, false>), grid, block, 0, s, b, hh, xx, ho, yy, stats);
-    else if (b.layer)
-        hipLaunchKernelGGL((norm_fwd_kernel<T, NT, C, false, true>), grid, block, 0, s, b, hh, xx, ho, yy, stats);
-    else
-        hipLaunchKernelGGL((norm_fwd_kernel<T, NT, C, false, false>), grid, block, 0, s, b, hh, xx, ho, yy, stats);
+        if (D <= 64 * W) f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
+    else if (D <= 128 * W) f(std::integral_constant<int, 128>(), std::integral_constant<int, 1>());
+    else if (D <= 256 * W) f(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
+    else if (D <= 512 * W) f(std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
+    else if (D <= 1024 * W) f(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
+    else if (D <= 2048 * W) f(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
+    else f(std::integral_constant<int, 1024>(), std::integral_constant<int, W == 8 ? 2 : 4>());
 }
 
 hipError_t block_norm_fwd(const BlockNorm& b, const void* h, const void* x, void* h_out, void* y,
                           float* stats, hipStream_t s)
 {
     if (b.rows == 0) return hipSuccess;
-    const bool vec = norm_vec(b, {h, x, h_out, y});
-    auto go = [&](auto t) {
+    const bool al = norm_vec(b, {h, x, h_out, y});
+    auto go = [&](auto t, auto layer, auto aligned) {
         using T = decltype(t);
-        if (b.D <= 512) launch_fwd<T, 64, 1>(b, vec, h, x, h_out, y, stats, s);
-        else if (b.D <= 1024) launch_fwd<T, 128, 1>(b, vec, h, x, h_out, y, stats, s);
-        else if (b.D <= 2048) launch_fwd<T, 256, 1>(b, vec, h, x, h_out, y, stats, s);
-        else if (b.D <= 4096) launch_fwd<T, 512, 1>(b, vec, h, x, h_out, y, stats, s);
-        else if (b.D <= 8192) launch_fwd<T, 1024, 1>(b, vec, h, x, h_out, y, stats, s);
-        else launch_fwd<T, 1024, 2>(b, vec, h, x, h_out, y, stats, s);
+        constexpr bool LAYER = decltype(layer)::value, AL = decltype(aligned)::value;
+        constexpr int W = kRun<T, LAYER, AL>;
+        with_row_shape<W>(b.D, [&](auto nt, auto c) {
+            constexpr int NT = decltype(nt)::value, C = decltype(c)::value;
+            constexpr int RPB = block_of(NT) / NT;
+            hipLaunchKernelGGL((norm_fwd_kernel<T, W, NT, C, AL, LAYER>),
+                               dim3((unsigned)((b.rows + RPB - 1) / RPB)), dim3(block_of(NT)), 0, s,
+                               b, static_cast<const T*>(h), static_cast<const T*>(x),
+                               static_cast<T*>(h_out), static_cast<T*>(y), stats);
+        });
     };
-    if (b.dt == DT_F32) go(float());
-    else go(bf16_t());
+    with_form(b, al, go);
     return hipGetLastError();
 }
 
@@ -239,28 +262,36 @@ hipError_t block_norm_fwd(const BlockNorm& b, const void* h, const void* x, void
 // into `pieces` pieces of `chunk` rows, or `gpb` whole groups make a block.
 struct NormDeal {
     long long group, groups_shard;   // rows of a group, groups of a shard
-    int pieces, chunk, gpb;
+    int pieces, chunk, gpb, Dp;      // Dp: D to a multiple of 4, the partial sums' rows
     long long blocks_shard, blocks;
 };
 
-static NormDeal norm_deal(const BlockNorm& b, int R)
+static NormDeal norm_deal(const BlockNorm& b, int R, bool al)
 {
     NormDeal q{};
     const long long nb = b.rows / R;
+    q.Dp = (b.D + 3) / 4 * 4;
     q.group = b.gate_rows ? b.gate_rows : nb;
     q.groups_shard = q.group ? nb / q.group : 0;
-    const long long target = std::max<long long>(1, 512 / R);   // blocks of a shard
-    const long long rows = std::max<long long>(1, (nb + target - 1) / target);
-    q.gpb = 1;
-    q.pieces = 1;
-    if (q.group > rows) {
-        q.pieces = (int)((q.group + rows - 1) / rows);
-        q.chunk = (int)((q.group + q.pieces - 1) / q.pieces);
-    } else {
-        q.gpb = (int)(q.group ? std::max<long long>(1, rows / q.group) : 1);
-        q.chunk = (int)q.group;
+    // At most the blocks that 256 compute units hold at 16 waves each (the kernels' registers):
+    // one more would run alone.  Fewer rows to a block than that gives only cost partial sums.
+    const int w = b.dt == DT_F32 || b.layer || !al ? 4 : 8;
+    int threads = 256;
+    while (threads < 1024 && threads * w < b.D) threads *= 2;
+    const long long slots = 256LL * 1024 / threads;
+    for (long long rows = std::max<long long>(1, nb * R / slots);; rows += std::max<long long>(1, rows / 16)) {
+        q.gpb = q.pieces = 1;
+        if (q.group > rows) {
+            q.pieces = (int)((q.group + rows - 1) / rows);
+            q.chunk = (int)((q.group + q.pieces - 1) / q.pieces);
+            q.blocks_shard = q.groups_shard * q.pieces;
+        } else {
+            q.gpb = (int)(q.group ? std::max<long long>(1, rows / q.group) : 1);
+            q.chunk = (int)q.group;
+            q.blocks_shard = (q.groups_shard + q.gpb - 1) / q.gpb;
+        }
+        if (q.blocks_shard * R <= slots || rows >= nb) break;
     }
-    q.blocks_shard = q.pieces > 1 ? q.groups_shard * q.pieces : (q.groups_shard + q.gpb - 1) / q.gpb;
     q.blocks = q.blocks_shard * R;
     return q;
 }
@@ -268,12 +299,12 @@ static NormDeal norm_deal(const BlockNorm& b, int R)
 // planes of a block's partial sums
 enum { PL_PRE_W, PL_POST_W, PL_GATE, PL_PRE_B, PL_POST_B, kPlanes };
 
-template <typename T, int NT, int C, bool VEC, bool LAYER>
-__global__ __launch_bounds__(block_of(NT)) void norm_bwd_kernel(BlockNorm b, BlockNormGrads g,
+template <typename T, int W, int NT, int C, bool AL, bool LAYER>
+__global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(BlockNorm b, BlockNormGrads g,
                                                                 NormDeal q, float* __restrict__ part)
 {
-    constexpr int N = 8 * C, RPB = block_of(NT) / NT;
-    __shared__ float red[2][2][16];
+    constexpr int N = W * C, RPB = block_of(NT) / NT, M = LAYER ? 2 : 1;
+    __shared__ float red[2][M][16];
     __shared__ float comb[RPB > 1 ? RPB - 1 : 1][RPB > 1 ? N * NT : 1];
     int slot = 0;
     const int l = threadIdx.x % NT, rs = threadIdx.x / NT, D = b.D;
@@ -320,31 +351,31 @@ __global__ __launch_bounds__(block_of(NT)) void norm_bwd_kernel(BlockNorm b, Blo
         for (int j0 = 0; j0 < rows; j0 += RPB) {
             const bool live = j0 + rs < rows;
             const long long i = base + (live ? j0 + rs : 0);
-            Raw<T, N, VEC> rH, ry, ro, rx;
-            Raw<float, N, VEC> rw;
+            Raw<T, N, AL> rH, ry, ro, rx;
+            Raw<float, N, AL> rw;
             float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
             if (g.stats) st = *reinterpret_cast<const float4*>(g.stats + 4 * i);
             float dH[N];
             if (has_y) {
-                load_raw<T, NT, C, VEC>(static_cast<const T*>(g.h_out) + i * b.ld_h, l, D, rH);
-                load_raw<T, NT, C, VEC>(static_cast<const T*>(g.dy) + i * b.ld_y, l, D, ry);
+                load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.h_out) + i * b.ld_h, l, D, rH);
+                load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.dy) + i * b.ld_y, l, D, ry);
             }
             if (g.dh_out)
-                load_raw<T, NT, C, VEC>(static_cast<const T*>(g.dh_out) + i * b.ld_h, l, D, ro);
-            if (has_x) load_raw<T, NT, C, VEC>(static_cast<const T*>(g.x) + i * b.ld_x, l, D, rx);
+                load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.dh_out) + i * b.ld_h, l, D, ro);
+            if (has_x) load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.x) + i * b.ld_x, l, D, rx);
 #pragma unroll
             for (int k = 0; k < N; ++k) dH[k] = g.dh_out ? raw_at(ro, k) : 0.f;
             if (has_y) {
-                load_raw<float, NT, C, VEC>(b.pre_w, l, D, rw);
-                float s[2] = {0.f, 0.f};
+                load_raw<float, NT, W, C, AL>(b.pre_w, l, D, rw);
+                float s[M] = {};
 #pragma unroll
                 for (int k = 0; k < N; ++k) {
                     const float p = raw_at(ry, k) * raw_at(rw, k);
                     s[0] = fmaf(p, (raw_at(rH, k) - st.z) * st.w, s[0]);
-                    if (LAYER) s[1] += p;
+                    if (LAYER) s[M - 1] += p;
                 }
-                row_sum<NT, 2>(s, red, slot);
-                const float c1 = s[0] * inv_d, c0 = LAYER ? s[1] * inv_d : 0.f;
+                row_sum<NT, M>(s, red, slot);
+                const float c1 = s[0] * inv_d, c0 = LAYER ? s[M - 1] * inv_d : 0.f;
 #pragma unroll
                 for (int k = 0; k < N; ++k) {
                     const float dy = raw_at(ry, k), hat = (raw_at(rH, k) - st.z) * st.w;
@@ -360,17 +391,17 @@ __global__ __launch_bounds__(block_of(NT)) void norm_bwd_kernel(BlockNorm b, Blo
                     float v[N];
 #pragma unroll
                     for (int k = 0; k < N; ++k) v[k] = raw_at(rH, k) > 0.f ? dH[k] : 0.f;
-                    store_row<T, NT, C, VEC>(static_cast<T*>(g.dh) + i * b.ld_h, l, D, v);
+                    store_row<T, NT, W, C, AL>(static_cast<T*>(g.dh) + i * b.ld_h, l, D, v);
                 } else {
-                    store_row<T, NT, C, VEC>(static_cast<T*>(g.dh) + i * b.ld_h, l, D, dH);
+                    store_row<T, NT, W, C, AL>(static_cast<T*>(g.dh) + i * b.ld_h, l, D, dH);
                 }
             }
             if (!has_x) continue;
             // du = scale gate dH; the gate's gradient is scale sum dH u
             float du[N];
             if (gate) {
-                Raw<float, N, VEC> rg;
-                load_raw<float, NT, C, VEC>(gate, l, D, rg);
+                Raw<float, N, AL> rg;
+                load_raw<float, NT, W, C, AL>(gate, l, D, rg);
 #pragma unroll
                 for (int k = 0; k < N; ++k) du[k] = b.scale * raw_at(rg, k) * dH[k];
             } else {
@@ -381,19 +412,19 @@ __global__ __launch_bounds__(block_of(NT)) void norm_bwd_kernel(BlockNorm b, Blo
                 if (live)
 #pragma unroll
                     for (int k = 0; k < N; ++k) gt[k] = fmaf(b.scale * dH[k], raw_at(rx, k), gt[k]);
-                if (g.dx && live) store_row<T, NT, C, VEC>(static_cast<T*>(g.dx) + i * b.ld_x, l, D, du);
+                if (g.dx && live) store_row<T, NT, W, C, AL>(static_cast<T*>(g.dx) + i * b.ld_x, l, D, du);
                 continue;
             }
-            load_raw<float, NT, C, VEC>(b.post_w, l, D, rw);
-            Raw<float, N, VEC> rb;
-            if (LAYER && b.post_b) load_raw<float, NT, C, VEC>(b.post_b, l, D, rb);
-            float s[2] = {0.f, 0.f};
+            load_raw<float, NT, W, C, AL>(b.post_w, l, D, rw);
+            Raw<float, N, AL> rb;
+            if (LAYER && b.post_b) load_raw<float, NT, W, C, AL>(b.post_b, l, D, rb);
+            float s[M] = {};
 #pragma unroll
             for (int k = 0; k < N; ++k) {
-                const float xh = elem<NT, VEC>(l, k) < D ? (raw_at(rx, k) - st.x) * st.y : 0.f;
+                const float xh = elem<NT, W, AL>(l, k) < D ? (raw_at(rx, k) - st.x) * st.y : 0.f;
                 const float p = du[k] * raw_at(rw, k);
                 s[0] = fmaf(p, xh, s[0]);
-                if (LAYER) s[1] += p;
+                if (LAYER) s[M - 1] += p;
                 if (live) {
                     float u = xh * raw_at(rw, k);
                     if (LAYER && b.post_b) u += raw_at(rb, k);
@@ -403,26 +434,26 @@ __global__ __launch_bounds__(block_of(NT)) void norm_bwd_kernel(BlockNorm b, Blo
                 }
             }
             if (!g.dx) continue;   // (the same in every thread)
-            row_sum<NT, 2>(s, red, slot);
-            const float c1 = s[0] * inv_d, c0 = LAYER ? s[1] * inv_d : 0.f;
+            row_sum<NT, M>(s, red, slot);
+            const float c1 = s[0] * inv_d, c0 = LAYER ? s[M - 1] * inv_d : 0.f;
 #pragma unroll
             for (int k = 0; k < N; ++k)
                 du[k] = st.y * (du[k] * raw_at(rw, k) - c0 - (raw_at(rx, k) - st.x) * st.y * c1);
-            if (live) store_row<T, NT, C, VEC>(static_cast<T*>(g.dx) + i * b.ld_x, l, D, du);
+            if (live) store_row<T, NT, W, C, AL>(static_cast<T*>(g.dx) + i * b.ld_x, l, D, du);
         }
         if (g.gate && b.gate_rows && q.pieces == 1) {   // the whole group was here
             combine(gt);
             if (rs == 0)
-                store_row<float, NT, C, VEC>(g.gate + (base / b.gate_rows) * D, l, D, gt);
+                store_row<float, NT, W, C, AL>(g.gate + (base / b.gate_rows) * D, l, D, gt);
 #pragma unroll
             for (int k = 0; k < N; ++k) gt[k] = 0.f;
         }
     }
-    float* out = part + (long long)blockIdx.x * kPlanes * D;
+    float* out = part + (long long)blockIdx.x * kPlanes * q.Dp;
     auto put = [&](bool wanted, int plane, float (&v)[N]) {
         if (!wanted) return;
         combine(v);
-        if (rs == 0) store_row<float, NT, C, VEC>(out + (long long)plane * D, l, D, v);
+        if (rs == 0) store_row<float, NT, W, C, AL>(out + (long long)plane * q.Dp, l, D, v);
     };
     put(g.pre_w, PL_PRE_W, pw);
     put(g.post_w, PL_POST_W, qw);
@@ -433,15 +464,16 @@ __global__ __launch_bounds__(block_of(NT)) void norm_bwd_kernel(BlockNorm b, Blo
     }
 }
 
-// The blocks' partial sums of one plane and shard (gate of a group: of the group's pieces), 64
-// columns to a block; its sixteen waves take runs of the blocks, joined in order.
+// The blocks' partial sums of one plane and shard (gate of a group: of the group's pieces), 256
+// columns to a block; its sixteen waves take runs of the partial sums, joined in order.
 __global__ __launch_bounds__(1024) void norm_join_kernel(BlockNormGrads g, NormDeal q, int R, int D,
                                                          bool group_gate,
                                                          const float* __restrict__ part)
 {
-    __shared__ float sum[16][64];
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    __shared__ f32x4 sum[16][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int d = blockIdx.y * 64 + lane;
+    const int d = blockIdx.y * 256 + lane * 4;
     long long o = blockIdx.x;   // which output row: shards x planes, then the groups' gates
     int plane;
     long long first, n;
@@ -463,67 +495,55 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(BlockNormGrads g, NormD
         n = q.pieces;
     }
     const long long per = (n + 15) / 16, b0 = w * per, b1 = min(n, b0 + per);
-    float v = 0.f;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if (d < D) {
-        const float* p = part + (first * kPlanes + plane) * D + d;
-#pragma unroll 4
-        for (long long k = b0; k < b1; ++k) v += p[k * kPlanes * D];
+        const f32x4* p = reinterpret_cast<const f32x4*>(part + (first * kPlanes + plane) * q.Dp + d);
+#pragma unroll 8
+        for (long long k = b0; k < b1; ++k) v += p[k * kPlanes * (q.Dp / 4)];
     }
     sum[w][lane] = v;
     __syncthreads();
     if (w || d >= D) return;
 #pragma unroll
     for (int k = 1; k < 16; ++k) v += sum[k][lane];
-    out[d] = v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (d + k < D) out[d + k] = v[k];
 }
 
 size_t block_norm_bwd_bytes(const BlockNorm& b, int R)
 {
-    return std::max<size_t>(256, (size_t)norm_deal(b, R).blocks * kPlanes * b.D * 4);
-}
-
-template <typename T, int NT, int C>
-static void launch_bwd(const BlockNorm& b, bool vec, const BlockNormGrads& g, const NormDeal& q,
-                       float* part, hipStream_t s)
-{
-    const dim3 grid((unsigned)q.blocks), block(block_of(NT));
-    if (vec && b.layer)
-        hipLaunchKernelGGL((norm_bwd_kernel<T, NT, C, true, true>), grid, block, 0, s, b, g, q, part);
-    else if (vec)
-        hipLaunchKernelGGL((norm_bwd_kernel<T, NT, C, true, false>), grid, block, 0, s, b, g, q, part);
-    else if (b.layer)
-        hipLaunchKernelGGL((norm_bwd_kernel<T, NT, C, false, true>), grid, block, 0, s, b, g, q, part);
-    else
-        hipLaunchKernelGGL((norm_bwd_kernel<T, NT, C, false, false>), grid, block, 0, s, b, g, q, part);
+    const NormDeal q = norm_deal(b, R, true), u = norm_deal(b, R, false);
+    return std::max<size_t>(256, (size_t)std::max(q.blocks, u.blocks) * kPlanes * q.Dp * 4);
 }
 
 hipError_t block_norm_bwd(const BlockNorm& b, int R, const BlockNormGrads& g, void* ws,
                           hipStream_t s)
 {
     float* part = static_cast<float*>(ws);
-    const NormDeal q = norm_deal(b, R);
     const bool group_gate = b.gate_rows != 0;
+    const bool al = norm_vec(b, {g.h_out, g.x, g.dy, g.dh_out, g.dh, g.dx,
+                                 group_gate ? g.gate : nullptr});
+    const NormDeal q = norm_deal(b, R, al);
     if (q.blocks) {
-        const bool vec = norm_vec(b, {g.h_out, g.x, g.dy, g.dh_out, g.dh, g.dx,
-                                      group_gate ? g.gate : nullptr});
-        auto go = [&](auto t) {
+        auto go = [&](auto t, auto layer, auto aligned) {
             using T = decltype(t);
-            if (b.D <= 512) launch_bwd<T, 64, 1>(b, vec, g, q, part, s);
-            else if (b.D <= 1024) launch_bwd<T, 128, 1>(b, vec, g, q, part, s);
-            else if (b.D <= 2048) launch_bwd<T, 256, 1>(b, vec, g, q, part, s);
-            else if (b.D <= 4096) launch_bwd<T, 512, 1>(b, vec, g, q, part, s);
-            else if (b.D <= 8192) launch_bwd<T, 1024, 1>(b, vec, g, q, part, s);
-            else launch_bwd<T, 1024, 2>(b, vec, g, q, part, s);
+            constexpr bool LAYER = decltype(layer)::value, AL = decltype(aligned)::value;
+            constexpr int W = kRun<T, LAYER, AL>;
+            with_row_shape<W>(b.D, [&](auto nt, auto c) {
+                constexpr int NT = decltype(nt)::value, C = decltype(c)::value;
+                hipLaunchKernelGGL((norm_bwd_kernel<T, W, NT, C, AL, LAYER>),
+                                   dim3((unsigned)q.blocks), dim3(block_of(NT)), 0, s, b, g, q, part);
+            });
         };
-        if (b.dt == DT_F32) go(float());
-        else go(bf16_t());
+        with_form(b, al, go);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (!g.pre_w && !g.post_w && !g.gate && !g.pre_b && !g.post_b) return hipSuccess;
     const long long rows = (long long)R * kPlanes +
                            (group_gate && g.gate && q.pieces > 1 ? q.groups_shard * R : 0);
-    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)rows, (b.D + 63) / 64), dim3(1024), 0, s, g,
+    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)rows, (b.D + 255) / 256), dim3(1024), 0, s, g,
                        q, R, b.D, group_gate, part);
     return hipGetLastError();
 }
