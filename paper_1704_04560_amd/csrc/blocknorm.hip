@@ -481,8 +481,8 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(BlockNormGrads g, NormD
     if (o < (long long)R * kPlanes) {
         plane = (int)(o / R);
         o %= R;
-        float* const outs[kPlanes] = {g.pre_w, g.post_w, group_gate ? nullptr : g.gate, g.pre_b, g.post_b};
-        out = outs[plane];
+        out = plane == PL_PRE_W ? g.pre_w : plane == PL_POST_W ? g.post_w : plane == PL_PRE_B ? g.pre_b
+              : plane == PL_POST_B ? g.post_b : group_gate ? nullptr : g.gate;
         if (!out) return;
         out += o * g.ld;
         first = o * q.blocks_shard;
@@ -498,8 +498,16 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(BlockNormGrads g, NormD
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if (d < D) {
         const f32x4* p = reinterpret_cast<const f32x4*>(part + (first * kPlanes + plane) * q.Dp + d);
-#pragma unroll 8
-        for (long long k = b0; k < b1; ++k) v += p[k * kPlanes * (q.Dp / 4)];
+        const long long step = kPlanes * (q.Dp / 4);
+        long long k = b0;
+        for (; k + 4 <= b1; k += 4) {
+            f32x4 t[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) t[j] = p[(k + j) * step];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v += t[j];
+        }
+        for (; k < b1; ++k) v += p[k * step];
     }
     sum[w][lane] = v;
     __syncthreads();
