@@ -439,7 +439,8 @@ int mtx_init_clip(const mtx_tensor* tensors, int count, void* workspace, size_t 
                 k.n = (unsigned)std::min(kClipChunk, t.n - o);
                 k.src_bf16 = t.src_type == MTX_BF16;
                 k.dst_bf16 = t.dst && t.dst_type == MTX_BF16;
-                k.vec = aligned(k.src, 16) && aligned(k.dst, 16);
+                k.src_vec = aligned(k.src, 16);
+                k.dst_vec = aligned(k.dst, 16);
                 table.push_back(k);
             }
         }

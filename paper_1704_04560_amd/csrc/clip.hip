@@ -7,6 +7,7 @@
 #include "internal.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace mtx {
 
@@ -42,8 +43,11 @@ __device__ __forceinline__ float clip_factor(const double* part, int np, const C
     return fin && norm > (double)o.max_norm ? (float)((double)o.max_norm / norm) : 1.0f;
 }
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
 template <bool EXACT>
-__global__ __launch_bounds__(256) void avg_sq_kernel(const float* __restrict__ grads, int R,
+__global__ __launch_bounds__(256) void avg_sq_scalar(const float* __restrict__ grads, int R,
                                                      long long n, long long ld,
                                                      float* __restrict__ avg,
                                                      double* __restrict__ part)
@@ -69,38 +73,173 @@ __global__ __launch_bounds__(256) void avg_sq_kernel(const float* __restrict__ g
     if (threadIdx.x == 0) part[blockIdx.x] = acc;
 }
 
+// 16-byte vectors, two per thread and pass, 4 KB apart; the rows are read once (nontemporal), the
+// average is read again by the second launch.  The n % 4 elements left over: the grid's first
+// thread.
+template <int RT, bool EXACT>
+__global__ __launch_bounds__(256) void avg_sq_vec4(const float* __restrict__ grads, int Rrt,
+                                                   long long n, long long ld,
+                                                   float* __restrict__ avg,
+                                                   double* __restrict__ part)
+{
+    typedef typename std::conditional<EXACT, double, float>::type A;
+    constexpr int U = 2;
+    __shared__ double red[4];
+    const int R = RT > 0 ? RT : Rrt;
+    const long long n4 = n / 4, ld4 = ld / 4;
+    const f32x4* g4 = reinterpret_cast<const f32x4*>(grads);
+    double acc = 0.0;
+    for (long long base = (long long)blockIdx.x * 256 * U; base < n4;
+         base += (long long)gridDim.x * 256 * U) {
+        A s[U][4];
+        bool ok[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            ok[u] = base + u * 256 + threadIdx.x < n4;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[u][j] = A(0);
+        }
+        auto row = [&](int r) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (ok[u]) {
+                    const f32x4 x = __builtin_nontemporal_load(g4 + r * ld4 + base + u * 256 + threadIdx.x);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[u][j] = r == 0 ? (A)x[j] : s[u][j] + (A)x[j];
+                }
+        };
+        if (RT > 0) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) row(r);
+        } else {
+            for (int r = 0; r < R; ++r) row(r);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!ok[u]) continue;
+            f32x4 g;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                g[j] = (float)(s[u][j] / (A)R);
+                acc = fma((double)g[j], (double)g[j], acc);
+            }
+            reinterpret_cast<f32x4*>(avg)[base + u * 256 + threadIdx.x] = g;
+        }
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0)
+        for (long long i = 4 * n4; i < n; ++i) {
+            A s = (A)grads[i];
+            for (int r = 1; r < R; ++r) s += (A)grads[(long long)r * ld + i];
+            const float g = (float)(s / (A)R);
+            avg[i] = g;
+            acc = fma((double)g, (double)g, acc);
+        }
+    acc = block_sum(acc, red);
+    if (threadIdx.x == 0) part[blockIdx.x] = acc;
+}
+
+// From the end of the vector to its start: what the first launch wrote last is still in the cache.
+template <bool VEC>
 __global__ __launch_bounds__(256) void scale_kernel(float* __restrict__ g, long long n,
                                                     const double* __restrict__ part, int np,
                                                     ClipOut o)
 {
     const float f = clip_factor(part, np, o);
     if (f == 1.0f) return;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n;
-         i += (long long)gridDim.x * 256)
-        g[i] *= f;
+    const long long step = (long long)gridDim.x * 256, n4 = VEC ? n / 4 : 0;
+    const long long t = (long long)blockIdx.x * 256 + threadIdx.x;
+    f32x4* g4 = reinterpret_cast<f32x4*>(g);
+#pragma unroll 2
+    for (long long i = n4 - 1 - t; i >= 0; i -= step) g4[i] *= f;
+    for (long long i = 4 * n4 + t; i < n; i += step) g[i] *= f;
+}
+
+template <bool EXACT>
+static void launch_avg_sq(const float* grads, int R, long long n, long long ld, float* avg,
+                          double* part, unsigned blocks, bool vec, hipStream_t s)
+{
+    // (LDS that keeps five blocks to a compute unit, as in the averages without a norm)
+    const size_t lds = 160 * 1024 / 5 - 1024;
+    auto go = [&](auto rt) {
+        hipLaunchKernelGGL((avg_sq_vec4<decltype(rt)::value, EXACT>), dim3(blocks), dim3(256), lds,
+                           s, grads, R, n, ld, avg, part);
+    };
+    if (!vec)
+        hipLaunchKernelGGL((avg_sq_scalar<EXACT>), dim3(blocks), dim3(256), 0, s, grads, R, n, ld,
+                           avg, part);
+    else if (R == 1) go(std::integral_constant<int, 1>());
+    else if (R == 2) go(std::integral_constant<int, 2>());
+    else if (R == 4) go(std::integral_constant<int, 4>());
+    else if (R == 8) go(std::integral_constant<int, 8>());
+    else if (R == 16) go(std::integral_constant<int, 16>());
+    else go(std::integral_constant<int, 0>());
 }
 
 hipError_t average_clip(const float* grads, int R, size_t n, size_t ld, bool exact, float max_norm,
                         float* avg, float* norm_out, int* nonfinite, double* part, hipStream_t s)
 {
-    const unsigned blocks = (unsigned)std::min<size_t>(kClipBlocks, (n + 255) / 256);
-    if (exact)
-        hipLaunchKernelGGL((avg_sq_kernel<true>), dim3(blocks), dim3(256), 0, s, grads, R,
-                           (long long)n, (long long)ld, avg, part);
-    else
-        hipLaunchKernelGGL((avg_sq_kernel<false>), dim3(blocks), dim3(256), 0, s, grads, R,
-                           (long long)n, (long long)ld, avg, part);
+    auto al = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
+    const bool vec_avg = al(avg), vec = vec_avg && al(grads) && ld % 4 == 0;
+    const size_t per = vec ? 2048 : 256;
+    const unsigned blocks = (unsigned)std::min<size_t>(kClipBlocks, (n + per - 1) / per);
+    if (exact) launch_avg_sq<true>(grads, R, n, ld, avg, part, blocks, vec, s);
+    else launch_avg_sq<false>(grads, R, n, ld, avg, part, blocks, vec, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const ClipOut o{max_norm, norm_out, nonfinite};
-    hipLaunchKernelGGL(scale_kernel, dim3(blocks), dim3(256), 0, s, avg, (long long)n, part,
-                       (int)blocks, o);
+    const unsigned sblocks = (unsigned)std::min<size_t>(kClipBlocks, (n + 1023) / 1024);
+    if (vec_avg)
+        hipLaunchKernelGGL((scale_kernel<true>), dim3(sblocks), dim3(256), 0, s, avg, (long long)n,
+                           part, (int)blocks, o);
+    else
+        hipLaunchKernelGGL((scale_kernel<false>), dim3(sblocks), dim3(256), 0, s, avg, (long long)n,
+                           part, (int)blocks, o);
     return hipGetLastError();
 }
 
 __device__ __forceinline__ float load_elem(const void* p, bool bf, unsigned i)
 {
     return bf ? bf16_to_f32(static_cast<const bf16_t*>(p)[i]) : static_cast<const float*>(p)[i];
+}
+
+__device__ __forceinline__ float word_at(u32x4 v, bool bf, int k)
+{
+    if (!bf) return __uint_as_float(v[k]);
+    return __uint_as_float(k % 2 ? v[k / 2] & 0xffff0000u : v[k / 2] << 16);
+}
+
+// The chunks' squares: 16-byte loads where the source is aligned, all of a thread's of a chunk in
+// flight together.
+template <bool BF>
+__device__ __forceinline__ double chunk_sq(const ClipChunk& k)
+{
+    constexpr int W = BF ? 8 : 4, U = 4;
+    double acc = 0.0;
+    unsigned done = 0;
+    if (k.src_vec) {
+        const u32x4* p = static_cast<const u32x4*>(k.src);
+        const unsigned nv = k.n / W;
+        for (unsigned i = threadIdx.x; i < nv; i += 256 * U) {
+            u32x4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                v[u] = i + u * 256 < nv ? p[i + u * 256] : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < W; ++j) {
+                    const double g = word_at(v[u], BF, j);
+                    acc = fma(g, g, acc);
+                }
+        }
+        done = nv * W;
+    }
+#pragma unroll 4
+    for (unsigned i = done + threadIdx.x; i < k.n; i += 256) {
+        const double g = load_elem(k.src, BF, i);
+        acc = fma(g, g, acc);
+    }
+    return acc;
 }
 
 __global__ __launch_bounds__(256) void list_sq_kernel(const ClipChunk* __restrict__ chunks,
@@ -110,15 +249,63 @@ __global__ __launch_bounds__(256) void list_sq_kernel(const ClipChunk* __restric
     double acc = 0.0;
     for (int c = blockIdx.x; c < count; c += gridDim.x) {
         const ClipChunk k = chunks[c];
-        for (unsigned i = threadIdx.x; i < k.n; i += 256) {
-            const double g = load_elem(k.src, k.src_bf16, i);
-            acc = fma(g, g, acc);
-        }
+        acc += k.src_bf16 ? chunk_sq<true>(k) : chunk_sq<false>(k);
     }
     acc = block_sum(acc, red);
     if (threadIdx.x == 0) part[blockIdx.x] = acc;
 }
 
+template <bool SB, bool DB>
+__device__ __forceinline__ void chunk_scale(const ClipChunk& k, float f)
+{
+    unsigned done = 0;
+    if (k.src_vec && k.dst_vec) {
+        const unsigned n8 = k.n / 8;   // eight elements at a time
+        const u32x4* p = static_cast<const u32x4*>(k.src);
+        u32x4* o = static_cast<u32x4*>(k.dst);
+#pragma unroll 2
+        for (unsigned i = threadIdx.x; i < n8; i += 256) {
+            float v[8];
+            if (SB) {
+                const u32x4 a = p[i];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = f * word_at(a, true, j);
+            } else {
+                const u32x4 a = p[2 * i], b = p[2 * i + 1];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[j] = f * word_at(a, false, j);
+                    v[4 + j] = f * word_at(b, false, j);
+                }
+            }
+            if (DB) {
+                u32x4 a;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    a[j] = f32_to_bf16(v[2 * j]) | (unsigned)f32_to_bf16(v[2 * j + 1]) << 16;
+                o[i] = a;
+            } else {
+                u32x4 a, b;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    a[j] = __float_as_uint(v[j]);
+                    b[j] = __float_as_uint(v[4 + j]);
+                }
+                o[2 * i] = a;
+                o[2 * i + 1] = b;
+            }
+        }
+        done = n8 * 8;
+    }
+#pragma unroll 4
+    for (unsigned i = done + threadIdx.x; i < k.n; i += 256) {
+        const float g = f * load_elem(k.src, SB, i);
+        if (DB) static_cast<bf16_t*>(k.dst)[i] = f32_to_bf16(g);
+        else static_cast<float*>(k.dst)[i] = g;
+    }
+}
+
+// From the list's end to its start, as scale_kernel.
 __global__ __launch_bounds__(256) void list_scale_kernel(const ClipChunk* __restrict__ chunks,
                                                          int count, bool all_in_place,
                                                          const double* __restrict__ part, int np,
@@ -126,14 +313,11 @@ __global__ __launch_bounds__(256) void list_scale_kernel(const ClipChunk* __rest
 {
     const float f = clip_factor(part, np, o);
     if (all_in_place && f == 1.0f) return;
-    for (int c = blockIdx.x; c < count; c += gridDim.x) {
+    for (int c = count - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
         const ClipChunk k = chunks[c];
         if (!k.dst || (k.dst == k.src && f == 1.0f)) continue;
-        for (unsigned i = threadIdx.x; i < k.n; i += 256) {
-            const float g = f * load_elem(k.src, k.src_bf16, i);
-            if (k.dst_bf16) static_cast<bf16_t*>(k.dst)[i] = f32_to_bf16(g);
-            else static_cast<float*>(k.dst)[i] = g;
-        }
+        if (k.src_bf16) k.dst_bf16 ? chunk_scale<true, true>(k, f) : chunk_scale<true, false>(k, f);
+        else k.dst_bf16 ? chunk_scale<false, true>(k, f) : chunk_scale<false, false>(k, f);
     }
 }
 

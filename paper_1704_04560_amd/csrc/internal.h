@@ -434,9 +434,9 @@ struct ClipChunk {
     const void* src;
     void* dst;
     unsigned n;
-    unsigned char src_bf16, dst_bf16, vec, pad;
+    unsigned char src_bf16, dst_bf16, src_vec, dst_vec;   // types; 16-byte aligned
 };
-constexpr size_t kClipChunk = 16384;
+constexpr size_t kClipChunk = 8192;
 hipError_t clip_list(const ClipChunk* chunks, int count, bool all_in_place, float max_norm,
                      float* norm_out, double* part, hipStream_t s);
 
