@@ -123,7 +123,7 @@ __global__ __launch_bounds__(256) void avg_sq_vec4(const float* __restrict__ gra
                 g[j] = (float)(s[u][j] / (A)R);
                 acc = fma((double)g[j], (double)g[j], acc);
             }
-            reinterpret_cast<f32x4*>(avg)[base + u * 256 + threadIdx.x] = g;
+            __builtin_nontemporal_store(g, reinterpret_cast<f32x4*>(avg) + base + u * 256 + threadIdx.x);
         }
     }
     if (blockIdx.x == 0 && threadIdx.x == 0)
@@ -181,7 +181,8 @@ hipError_t average_clip(const float* grads, int R, size_t n, size_t ld, bool exa
     auto al = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
     const bool vec_avg = al(avg), vec = vec_avg && al(grads) && ld % 4 == 0;
     const size_t per = vec ? 2048 : 256;
-    const unsigned blocks = (unsigned)std::min<size_t>(kClipBlocks, (n + per - 1) / per);
+    // five blocks to each of 256 compute units: more would run as a second, partly filled round
+    const unsigned blocks = (unsigned)std::min<size_t>(vec ? 1280 : kClipBlocks, (n + per - 1) / per);
     if (exact) launch_avg_sq<true>(grads, R, n, ld, avg, part, blocks, vec, s);
     else launch_avg_sq<false>(grads, R, n, ld, avg, part, blocks, vec, s);
     const hipError_t e = hipGetLastError();
@@ -247,8 +248,11 @@ __global__ __launch_bounds__(256) void list_sq_kernel(const ClipChunk* __restric
 {
     __shared__ double red[4];
     double acc = 0.0;
+    ClipChunk next{};
+    if ((int)blockIdx.x < count) next = chunks[blockIdx.x];
     for (int c = blockIdx.x; c < count; c += gridDim.x) {
-        const ClipChunk k = chunks[c];
+        const ClipChunk k = next;
+        if (c + (int)gridDim.x < count) next = chunks[c + gridDim.x];
         acc += k.src_bf16 ? chunk_sq<true>(k) : chunk_sq<false>(k);
     }
     acc = block_sum(acc, red);
