@@ -439,8 +439,9 @@ int mtx_init_clip(const mtx_tensor* tensors, int count, void* workspace, size_t 
                 k.n = (unsigned)std::min(kClipChunk, t.n - o);
                 k.src_bf16 = t.src_type == MTX_BF16;
                 k.dst_bf16 = t.dst && t.dst_type == MTX_BF16;
-                k.src_vec = aligned(k.src, 16);
-                k.dst_vec = aligned(k.dst, 16);
+                const size_t ea = k.dst ? ed : es;
+                const size_t off = reinterpret_cast<uintptr_t>(k.dst ? k.dst : k.src) % 16;
+                k.head = (unsigned char)std::min<size_t>(k.n, off ? (16 - off) / ea : 0);
                 table.push_back(k);
             }
         }

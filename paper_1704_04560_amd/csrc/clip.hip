@@ -209,37 +209,38 @@ __device__ __forceinline__ float word_at(u32x4 v, bool bf, int k)
     return __uint_as_float(k % 2 ? v[k / 2] & 0xffff0000u : v[k / 2] << 16);
 }
 
-// The chunks' squares: 16-byte loads where the source is aligned, all of a thread's of a chunk in
-// flight together.
-template <bool BF>
-__device__ __forceinline__ double chunk_sq(const ClipChunk& k)
+// 16 bytes at any element: a source need not be aligned where its destination is.
+template <bool BF> struct AnyVec { typedef unsigned type __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct AnyVec<true> { typedef unsigned type __attribute__((ext_vector_type(4), aligned(2))); };
+
+// The elements of a chunk that belong to no whole vector of W: its head and its end.
+template <class F> __device__ __forceinline__ void chunk_rest(const ClipChunk& k, unsigned end, F f)
+{
+    if (threadIdx.x < k.head) f(threadIdx.x);
+    if (end + threadIdx.x < k.n) f(end + threadIdx.x);
+}
+
+template <bool BF> __device__ __forceinline__ double chunk_sq(const ClipChunk& k)
 {
     constexpr int W = BF ? 8 : 4, U = 4;
+    typedef typename AnyVec<BF>::type V;
     double acc = 0.0;
-    unsigned done = 0;
-    if (k.src_vec) {
-        const u32x4* p = static_cast<const u32x4*>(k.src);
-        const unsigned nv = k.n / W;
-        for (unsigned i = threadIdx.x; i < nv; i += 256 * U) {
-            u32x4 v[U];
+    auto add = [&](float x) { acc = fma((double)x, (double)x, acc); };
+    const V* p = reinterpret_cast<const V*>(static_cast<const char*>(k.src) + k.head * (BF ? 2 : 4));
+    const unsigned nv = (k.n - k.head) / W;
+    for (unsigned i = threadIdx.x; i < nv; i += 256 * U) {
+        u32x4 v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                v[u] = i + u * 256 < nv ? p[i + u * 256] : u32x4{0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int j = 0; j < W; ++j) {
-                    const double g = word_at(v[u], BF, j);
-                    acc = fma(g, g, acc);
-                }
+        for (int u = 0; u < U; ++u) {
+            v[u] = u32x4{0u, 0u, 0u, 0u};
+            if (i + u * 256 < nv) v[u] = p[i + u * 256];
         }
-        done = nv * W;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < W; ++j) add(word_at(v[u], BF, j));
     }
-#pragma unroll 4
-    for (unsigned i = done + threadIdx.x; i < k.n; i += 256) {
-        const double g = load_elem(k.src, BF, i);
-        acc = fma(g, g, acc);
-    }
+    chunk_rest(k, k.head + nv * W, [&](unsigned i) { add(load_elem(k.src, BF, i)); });
     return acc;
 }
 
@@ -259,54 +260,58 @@ __global__ __launch_bounds__(256) void list_sq_kernel(const ClipChunk* __restric
     if (threadIdx.x == 0) part[blockIdx.x] = acc;
 }
 
+// 16 bytes of dst at a time: whole aligned vectors, next to each other in a wave, written past the
+// caches (291 tensors bf16 -> fp32 at odd places of one vector, both launches: single elements
+// through the caches 117 us; past them 120, half-line vectors 108, whole ones 88).
 template <bool SB, bool DB>
 __device__ __forceinline__ void chunk_scale(const ClipChunk& k, float f)
 {
-    unsigned done = 0;
-    if (k.src_vec && k.dst_vec) {
-        const unsigned n8 = k.n / 8;   // eight elements at a time
-        const u32x4* p = static_cast<const u32x4*>(k.src);
-        u32x4* o = static_cast<u32x4*>(k.dst);
-#pragma unroll 2
-        for (unsigned i = threadIdx.x; i < n8; i += 256) {
-            float v[8];
-            if (SB) {
-                const u32x4 a = p[i];
+    constexpr int W = DB ? 8 : 4, U = 2;
+    constexpr int SW = W * (SB ? 2 : 4) / 4;   // words of the source
+    typedef unsigned pair_t __attribute__((ext_vector_type(2), aligned(2)));
+    typedef typename AnyVec<SB>::type V;
+    const char* p = static_cast<const char*>(k.src) + k.head * (SB ? 2 : 4);
+    u32x4* o = reinterpret_cast<u32x4*>(static_cast<char*>(k.dst) + k.head * (DB ? 2 : 4));
+    const unsigned nv = (k.n - k.head) / W;
+    for (unsigned i = threadIdx.x; i < nv; i += 256 * U) {
+        unsigned w[U][SW];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = f * word_at(a, true, j);
+        for (int u = 0; u < U; ++u) {
+            if (i + u * 256 >= nv) continue;
+            const char* q = p + (size_t)(i + u * 256) * SW * 4;
+            if constexpr (SW == 2) {
+                const pair_t h = *reinterpret_cast<const pair_t*>(q);
+                w[u][0] = h[0];
+                w[u][1] = h[1];
             } else {
-                const u32x4 a = p[2 * i], b = p[2 * i + 1];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    v[j] = f * word_at(a, false, j);
-                    v[4 + j] = f * word_at(b, false, j);
+                for (int j = 0; j < SW; j += 4) {
+                    const u32x4 h = *reinterpret_cast<const V*>(q + j * 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[u][j + e] = h[e];
                 }
-            }
-            if (DB) {
-                u32x4 a;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    a[j] = f32_to_bf16(v[2 * j]) | (unsigned)f32_to_bf16(v[2 * j + 1]) << 16;
-                o[i] = a;
-            } else {
-                u32x4 a, b;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    a[j] = __float_as_uint(v[j]);
-                    b[j] = __float_as_uint(v[4 + j]);
-                }
-                o[2 * i] = a;
-                o[2 * i + 1] = b;
             }
         }
-        done = n8 * 8;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i + u * 256 >= nv) continue;
+            float v[W];
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                v[j] = f * __uint_as_float(!SB ? w[u][j] : j % 2 ? w[u][j / 2] & 0xffff0000u : w[u][j / 2] << 16);
+            u32x4 r;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                r[j] = DB ? f32_to_bf16(v[2 * j % W]) | (unsigned)f32_to_bf16(v[(2 * j + 1) % W]) << 16
+                          : __float_as_uint(v[j]);
+            __builtin_nontemporal_store(r, o + i + u * 256);
+        }
     }
-#pragma unroll 4
-    for (unsigned i = done + threadIdx.x; i < k.n; i += 256) {
+    chunk_rest(k, k.head + nv * W, [&](unsigned i) {
         const float g = f * load_elem(k.src, SB, i);
         if (DB) static_cast<bf16_t*>(k.dst)[i] = f32_to_bf16(g);
         else static_cast<float*>(k.dst)[i] = g;
-    }
+    });
 }
 
 // From the list's end to its start, as scale_kernel.

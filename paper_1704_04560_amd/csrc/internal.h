@@ -429,12 +429,13 @@ constexpr int kClipBlocks = 2048;
 // as average_adapt does); norm_out, nonfinite (set to 0 or 1) nullable.
 hipError_t average_clip(const float* grads, int R, size_t n, size_t ld, bool exact, float max_norm,
                         float* avg, float* norm_out, int* nonfinite, double* part, hipStream_t s);
-// One piece of a tensor of the list: n elements.
+// One piece of a tensor of the list: n elements, `head` of them before the first 16-byte aligned one
+// of dst (of src without a dst).
 struct ClipChunk {
     const void* src;
     void* dst;
     unsigned n;
-    unsigned char src_bf16, dst_bf16, src_vec, dst_vec;   // types; 16-byte aligned
+    unsigned char src_bf16, dst_bf16, head, pad;
 };
 constexpr size_t kClipChunk = 8192;
 hipError_t clip_list(const ClipChunk* chunks, int count, bool all_in_place, float max_norm,
