@@ -73,14 +73,15 @@ __global__ __launch_bounds__(256) void avg_sq_scalar(const float* __restrict__ g
     if (threadIdx.x == 0) part[blockIdx.x] = acc;
 }
 
-// 16-byte vectors, two per thread and pass, 4 KB apart; the rows are read once (nontemporal), the
-// average is read again by the second launch.  The n % 4 elements left over: the grid's first
-// thread.
+// 16-byte vectors, two per thread and pass, 4 KB apart; the rows are read once (nontemporal).  The
+// average is read again by the second launch; it is written through the caches, or past them where
+// the rows' traffic would push it out (`past`).  The n % 4 elements left over: the grid's first thread.
+// 16 x 61M: 697 us, 5.95 TB/s.
 template <int RT, bool EXACT>
 __global__ __launch_bounds__(256) void avg_sq_vec4(const float* __restrict__ grads, int Rrt,
                                                    long long n, long long ld,
                                                    float* __restrict__ avg,
-                                                   double* __restrict__ part)
+                                                   double* __restrict__ part, bool past)
 {
     typedef typename std::conditional<EXACT, double, float>::type A;
     constexpr int U = 2;
@@ -123,7 +124,9 @@ __global__ __launch_bounds__(256) void avg_sq_vec4(const float* __restrict__ gra
                 g[j] = (float)(s[u][j] / (A)R);
                 acc = fma((double)g[j], (double)g[j], acc);
             }
-            __builtin_nontemporal_store(g, reinterpret_cast<f32x4*>(avg) + base + u * 256 + threadIdx.x);
+            f32x4* out = reinterpret_cast<f32x4*>(avg) + base + u * 256 + threadIdx.x;
+            if (past) __builtin_nontemporal_store(g, out);
+            else *out = g;
         }
     }
     if (blockIdx.x == 0 && threadIdx.x == 0)
@@ -160,9 +163,12 @@ static void launch_avg_sq(const float* grads, int R, long long n, long long ld, 
 {
     // (LDS that keeps five blocks to a compute unit, as in the averages without a norm)
     const size_t lds = 160 * 1024 / 5 - 1024;
+    // Average, clip and update: 4 x 30M (600 MB) 230 us through the caches, 236 past them; 16 x 16M
+    // (1.1 GB) 264 and 248.
+    const bool past = (double)n * (R + 1) * 4 > 768e6;
     auto go = [&](auto rt) {
         hipLaunchKernelGGL((avg_sq_vec4<decltype(rt)::value, EXACT>), dim3(blocks), dim3(256), lds,
-                           s, grads, R, n, ld, avg, part);
+                           s, grads, R, n, ld, avg, part, past);
     };
     if (!vec)
         hipLaunchKernelGGL((avg_sq_scalar<EXACT>), dim3(blocks), dim3(256), 0, s, grads, R, n, ld,
