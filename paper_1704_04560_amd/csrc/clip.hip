@@ -75,13 +75,13 @@ __global__ __launch_bounds__(256) void avg_sq_scalar(const float* __restrict__ g
 
 // 16-byte vectors, two per thread and pass, 4 KB apart; the rows are read once (nontemporal).  The
 // average is read again by the second launch; it is written through the caches, or past them where
-// the rows' traffic would push it out (`past`).  The n % 4 elements left over: the grid's first thread.
+// the rows' traffic would push it out (PAST).  The n % 4 elements left over: the grid's first thread.
 // 16 x 61M: 697 us, 5.95 TB/s.
-template <int RT, bool EXACT>
+template <int RT, bool EXACT, bool PAST>
 __global__ __launch_bounds__(256) void avg_sq_vec4(const float* __restrict__ grads, int Rrt,
                                                    long long n, long long ld,
                                                    float* __restrict__ avg,
-                                                   double* __restrict__ part, bool past)
+                                                   double* __restrict__ part)
 {
     typedef typename std::conditional<EXACT, double, float>::type A;
     constexpr int U = 2;
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(256) void avg_sq_vec4(const float* __restrict__ gra
                 acc = fma((double)g[j], (double)g[j], acc);
             }
             f32x4* out = reinterpret_cast<f32x4*>(avg) + base + u * 256 + threadIdx.x;
-            if (past) __builtin_nontemporal_store(g, out);
+            if (PAST) __builtin_nontemporal_store(g, out);
             else *out = g;
         }
     }
@@ -167,8 +167,13 @@ static void launch_avg_sq(const float* grads, int R, long long n, long long ld, 
     // (1.1 GB) 264 and 248.
     const bool past = (double)n * (R + 1) * 4 > 768e6;
     auto go = [&](auto rt) {
-        hipLaunchKernelGGL((avg_sq_vec4<decltype(rt)::value, EXACT>), dim3(blocks), dim3(256), lds,
-                           s, grads, R, n, ld, avg, part, past);
+        constexpr int RT = decltype(rt)::value;
+        if (past)
+            hipLaunchKernelGGL((avg_sq_vec4<RT, EXACT, true>), dim3(blocks), dim3(256), lds, s,
+                               grads, R, n, ld, avg, part);
+        else
+            hipLaunchKernelGGL((avg_sq_vec4<RT, EXACT, false>), dim3(blocks), dim3(256), lds, s,
+                               grads, R, n, ld, avg, part);
     };
     if (!vec)
         hipLaunchKernelGGL((avg_sq_scalar<EXACT>), dim3(blocks), dim3(256), 0, s, grads, R, n, ld,
