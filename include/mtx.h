@@ -59,7 +59,9 @@ typedef enum {
     MTX_MAXPOOL = 2,
     MTX_BN = 3,
     MTX_ADD = 4,
-    MTX_ADDP = 5
+    MTX_ADDP = 5,
+    MTX_EMBED = 6,
+    MTX_NORM = 7
 } mtx_kind;
 
 /* One layer (Sec. I and Fig. 1: fully connected and convolution layers; pooling between
@@ -85,6 +87,17 @@ typedef enum {
  *                count of x; parameters W[out][channels of a_k] and b[out], Glorot-initialised
  *                as a convolution's.  P is a stored output (bf16 in MTX_BF16 mode) before the
  *                addition; a layer is the source of at most one addition; relu as above.
+ *   MTX_EMBED:   token embedding, the first layer only: the input shape is 1 x h x w, one token per
+ *                position (given to mtx_train_step_tokens), and the output out x h x w, the row of
+ *                the table W[k][out] that a token names (k = the number of tokens; no bias),
+ *                times the scale of mtx_set_embedding.  W is Glorot-initialised with fan_in = k,
+ *                fan_out = out.  groups 0 or 1, stride 0 or 1, pad and relu 0.
+ *   MTX_NORM:    normalisation of each position over its channels (eps = 1e-5): k = MTX_NORM_LAYER
+ *                (mean and variance; parameters gamma[c] in the place of W, beta[c] in the place
+ *                of b) or MTX_NORM_RMS (mean square; gamma alone), gamma 1 and beta 0 at the
+ *                start; out 0 or the channel count (at most 16384), stride and groups 0 or 1, pad
+ *                and relu 0.  After an MTX_ADD without ReLU it is computed in the addition's pass,
+ *                from the sum before it is rounded.
  * The last layer must be MTX_FC without ReLU; its outputs are the class scores of a softmax
  * cross-entropy loss. */
 typedef struct {
@@ -170,6 +183,18 @@ int mtx_init_model_static(const mtx_model_desc* desc, int R, int shard_batch, ui
 int mtx_train_step(mtx_model* m, const float* x, const int32_t* labels, float lr,
                    float momentum, float* loss_out, void* stream);
 
+/* The same step of a network whose first layer is MTX_EMBED: tokens [B][in_h][in_w] int32, 4-byte
+ * aligned, in the place of x.  A token outside the table gives a NaN output (and so a NaN loss),
+ * and takes no part in the table's gradient.  Each of the two calls returns MTX_EINVAL for a
+ * network of the other kind. */
+int mtx_train_step_tokens(mtx_model* m, const int32_t* tokens, const int32_t* labels, float lr,
+                          float momentum, float* loss_out, void* stream);
+
+/* Scale (finite, default 1) of the outputs of a model's MTX_EMBED layer, and its padding token
+ * (default -1: none), whose output is zero and which takes no part in the table's gradient.
+ * MTX_EINVAL for a model without that layer. */
+int mtx_set_embedding(mtx_model* m, float scale, int pad);
+
 /* avg[i] = (1/R) sum_{r<R} grads[r*ld + i] for i < n: the averaging of replica gradients
  * (Sec. II-B, III-D.2) over R buffers held on this GPU.  Requires R >= 1, n >= 1, ld >= n;
  * avg must not overlap grads.  Asynchronous. */
@@ -253,6 +278,18 @@ int mtx_set_overlap(mtx_model* m, int enable);
  * for a NULL model. */
 int mtx_set_nonfinite_check(mtx_model* m, int enable);
 
+/* Clipping of the averaged gradient by its global norm (option, default off).  With max_norm > 0
+ * (infinity: the norm is computed, nothing is clipped), mtx_train_step averages the R shard
+ * gradients into grad_avg with their norm, scales grad_avg by max_norm / norm where the norm
+ * exceeds max_norm (as mtx_average_clip does; a norm that is not finite clips nothing), and
+ * applies the update rule, any of mtx_set_optimizer's, from grad_avg.  norm_out (nullable, device
+ * fp32 [1]) receives the norm before clipping at every step; workspace is
+ * MTX_CLIP_WORKSPACE_BYTES of device scratch, 16-byte aligned; both are the caller's, stay in
+ * use until the option is set again, and overlap no model buffer.  The fused and layer-wise
+ * updates are not used while it is on.  max_norm = 0 switches it off (the other arguments are
+ * then ignored). */
+int mtx_set_clip_norm(mtx_model* m, float max_norm, float* norm_out, void* workspace);
+
 /* Fused average + update of large fully connected layers (execution option, default on).  With
  * the momentum rule (not Adam or AdaGrad) and without the layer-wise option, a fully connected
  * layer of at least 2^20 parameters whose weight gradient has at least 512 output tiles of
@@ -306,7 +343,10 @@ int mtx_set_optimizer(mtx_model* m, int kind, float beta1, float beta2, float ep
  * of its own; "add_bwd" runs only where the previous layer's gradient is not the addition's
  * own buffer; "skip_add" adds a shortcut's share into its source's gradient); "fwd_direct" and
  * "wgrad_direct" for a first convolution of one input channel and a 3x3, 5x5 or 7x7 window
- * (at most 32 outputs), which runs on direct kernels instead of the matrix kernels; the second
+ * (at most 32 outputs), which runs on direct kernels instead of the matrix kernels; "embed_fwd",
+ * "embed_bwd" (with "_gather" and "_join"), "norm_fwd" and "norm_bwd" (with "_join") for token
+ * embeddings and norms (an addition computed with the norm after it has no site of its own), and
+ * "avg_clip" (with "_scale") for the average of a clipped step; the second
  * kernel of an operation is a site of its own: "<site>_reduce" (the second pass of a split
  * reduction), "dgrad_col2im", "bn_fwd_finalize" / "bn_bwd_finalize" (per-channel statistics
  * from the partial sums) and "bn_fwd_apply" / "bn_bwd_apply" (the elementwise pass after the

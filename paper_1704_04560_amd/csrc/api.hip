@@ -77,6 +77,8 @@ struct LayerPlan {
     size_t skip_off;             // projection shortcut: gradient for the source layer [B][...]
     bool skip_compact;           // ... only at the positions that the strided projection reads
     size_t proj_off;             // projection shortcut: its stored output [B][oh][ow][oc]
+    int norm;                    // MTX_NORM: mtx_norm_kind
+    int vocab;                   // MTX_EMBED: rows of the table
     bool dy_shared;              // residual addition: the previous layer's output gradient is
                                  // this layer's own buffer (no copy is made)
 };
@@ -101,11 +103,30 @@ struct Plan {
     size_t xin_off = 0, xin_bytes = 0, prep_off = 0, jobs_off = 0, loss_off = 0;
     size_t partial_off = 0, partial_w_off = 0, col_off = 0, sync_off = 0;
     size_t bn_part_off = 0, bn_coef_off = 0;  // batch normalisation scratch
+    size_t ops_off = 0;          // scratch of the embedding's and the norms' gradients
     size_t first_part_off = 0;                 // direct first convolution: per-image sums
     int n_wgrad = 0;             // layers with a weight gradient
     double gemm_flops = 0;       // multiply-adds x 2 of every matrix launch of a step
     size_t ws_bytes = 0;
 };
+
+constexpr float kNormEps = 1e-5f;  // MTX_NORM
+
+// MTX_NORM layer over N images (R shards of them).
+BlockNorm norm_args(const LayerPlan& lp, int dt, long long N, const float* gamma, const float* beta)
+{
+    BlockNorm b{};
+    b.layer = lp.norm == MTX_NORM_LAYER;
+    b.dt = (Dt)dt;
+    b.rows = N * lp.h * lp.w;
+    b.D = lp.c;
+    b.eps = kNormEps;
+    b.scale = 1.0f;
+    b.pre_w = gamma;
+    b.pre_b = b.layer ? beta : nullptr;
+    b.ld_h = b.ld_x = b.ld_y = lp.c;
+    return b;
+}
 
 constexpr double kOverlapFlops = 50e9;  // matrix work of a step from which its streams overlap
 
@@ -226,6 +247,34 @@ int plan_with(const mtx_model_desc* d, int R, int Nb, bool halo, Plan& pl)
             lp.src = src;
             lp.k = 1; lp.p = 0; lp.g = 1;
             lp.oc = c; lp.oh = h; lp.ow = w;
+        } else if (ly.kind == MTX_EMBED) {
+            if (i != 0 || c != 1)
+                return fail(MTX_EINVAL, "layer %d: an embedding is the first layer, of one input "
+                                        "channel", i);
+            if (ly.out < 1 || ly.k < 1 || ly.pad != 0 || ly.relu ||
+                (ly.stride != 0 && ly.stride != 1) || (ly.groups != 0 && ly.groups != 1))
+                return fail(MTX_EINVAL, "layer %d: an embedding takes only out and k (tokens)", i);
+            if ((long long)ly.k * R > (1LL << 28) || (long long)h * w * B > (1LL << 30) || R > 65536)
+                return fail(MTX_EINVAL, "layer %d: the embedding is too large", i);
+            lp.k = 1; lp.s = 1; lp.p = 0; lp.g = 1;
+            lp.vocab = ly.k;
+            lp.oc = ly.out; lp.oh = h; lp.ow = w;
+            lp.w_len = (size_t)ly.k * ly.out;
+            lp.b_len = 0;
+        } else if (ly.kind == MTX_NORM) {
+            if ((ly.out != 0 && ly.out != c) || (ly.k != MTX_NORM_RMS && ly.k != MTX_NORM_LAYER) ||
+                ly.pad != 0 || ly.relu || (ly.stride != 0 && ly.stride != 1) ||
+                (ly.groups != 0 && ly.groups != 1))
+                return fail(MTX_EINVAL, "layer %d: a norm takes only k, its kind (out, if given, "
+                                        "must be its channel count)", i);
+            if (c > kNormMaxD)
+                return fail(MTX_EUNSUPPORTED, "layer %d: a norm of %d channels (at most %d)", i, c,
+                            kNormMaxD);
+            lp.k = 1; lp.s = 1; lp.p = 0; lp.g = 1;
+            lp.norm = ly.k;
+            lp.oc = c; lp.oh = h; lp.ow = w;
+            lp.w_len = c;
+            lp.b_len = ly.k == MTX_NORM_LAYER ? c : 0;
         } else {
             return fail(MTX_EINVAL, "layer %d: unknown kind %d", i, ly.kind);
         }
@@ -251,7 +300,7 @@ int plan_with(const mtx_model_desc* d, int R, int Nb, bool halo, Plan& pl)
         lp.need_dx = (int)i > pl.first_param && pl.first_param >= 0;
         // a pooled tensor that feeds a fully connected layer is stored NCHW
         lp.nhwc = lp.kind == MTX_CONV || lp.kind == MTX_BN || lp.kind == MTX_ADD ||
-                  lp.kind == MTX_ADDP ||
+                  lp.kind == MTX_ADDP || lp.kind == MTX_EMBED || lp.kind == MTX_NORM ||
                   (lp.kind == MTX_MAXPOOL && !(i + 1 < pl.L.size() && pl.L[i + 1].kind == MTX_FC));
         lp.perm_c = 1;
         lp.perm_hw = 1;
@@ -270,7 +319,8 @@ int plan_with(const mtx_model_desc* d, int R, int Nb, bool halo, Plan& pl)
         pl.x_c = pl.in_c;
         pl.x_hw = pl.in_h * pl.in_w;
     }
-    pl.x_convert = pl.dt == MTX_BF16 || (pl.x_c > 1 && pl.x_hw > 1);
+    pl.x_convert = first.kind != MTX_EMBED &&
+                   (pl.dt == MTX_BF16 || (pl.x_c > 1 && pl.x_hw > 1));
     // A first convolution whose channel count rules out 16-byte loads reads a padded input
     // instead (see conv_fwd_run), when that adds at most 3x to its multiply-adds.
     first.run = false;
@@ -314,7 +364,7 @@ int plan_with(const mtx_model_desc* d, int R, int Nb, bool halo, Plan& pl)
         if (lp.w_len && lp.kind == MTX_ADDP) {
             const double macs = (double)pl.B * lp.oh * lp.ow * lp.oc * pl.L[lp.src].oc;
             pl.gemm_flops += 2.0 * macs * (lp.src >= pl.first_param ? 3 : 2);
-        } else if (lp.w_len && lp.kind != MTX_BN) {
+        } else if (lp.kind == MTX_CONV || lp.kind == MTX_FC) {
             const double macs = lp.kind == MTX_CONV
                                     ? (double)pl.B * lp.oh * lp.ow * lp.oc * (lp.c / lp.g) * lp.k * lp.k
                                     : (double)pl.B * lp.in_elems * lp.oc;
@@ -341,7 +391,8 @@ int plan_with(const mtx_model_desc* d, int R, int Nb, bool halo, Plan& pl)
     for (size_t i = 0; i < pl.L.size(); ++i) {
         LayerPlan& lp = pl.L[i];
         lp.fw_off = lp.bw_off = kNone;
-        if (!lp.w_len || lp.kind == MTX_BN) continue;  // BN reads gamma and beta as they are
+        // (norms and embeddings read their fp32 parameters as they are)
+        if (!lp.w_len || lp.kind == MTX_BN || lp.kind == MTX_NORM || lp.kind == MTX_EMBED) continue;
         PrepJob j{};
         j.n = (int)lp.w_len;
         j.src = (long long)lp.w_off;
@@ -430,7 +481,7 @@ int plan_with(const mtx_model_desc* d, int R, int Nb, bool halo, Plan& pl)
     // fp32 partial sums: one region for the forward and data-gradient launches, one for the
     // weight gradients (which may run concurrently on a second stream)
     size_t max_partial = 0, max_partial_w = 0, max_col = 0, max_bn_part = 0, max_bn_coef = 0;
-    size_t max_first = 0;
+    size_t max_first = 0, max_ops = 0;
     for (size_t i = 0; i < pl.L.size(); ++i) {
         LayerPlan& lp = pl.L[i];
         lp.act_f32 = (pl.dt == MTX_F32) || (i + 1 == pl.L.size());
@@ -451,6 +502,13 @@ int plan_with(const mtx_model_desc* d, int R, int Nb, bool halo, Plan& pl)
                                                                    lp.h * lp.w));
             max_bn_coef = std::max(max_bn_coef, (size_t)pl.R * lp.c * 3);
         }
+        if (lp.kind == MTX_NORM) {   // mean and 1 / std of each position (see mtx_block_norm_forward)
+            lp.stat_off = ws;
+            ws = align_up(ws + (size_t)pl.B * lp.h * lp.w * 16, kAlign);
+            max_ops = std::max(max_ops, block_norm_bwd_bytes(norm_args(lp, pl.dt, pl.B, nullptr, nullptr), R));
+        }
+        if (lp.kind == MTX_EMBED)
+            max_ops = std::max(max_ops, embed_bwd_bytes((long long)pl.Nb * lp.h * lp.w, R, lp.vocab, lp.oc));
         // a projection shortcut keeps the gradient for its source (its data gradient) until the
         // source's own output gradient exists (only when the source's gradient is needed at
         // all); an identity addition's share is its own output gradient, which stays unchanged
@@ -569,6 +627,8 @@ int plan_with(const mtx_model_desc* d, int R, int Nb, bool halo, Plan& pl)
     ws = align_up(ws + max_first * 4, kAlign);
     pl.bn_coef_off = ws;
     ws = align_up(ws + max_bn_coef * 4, kAlign);
+    pl.ops_off = ws;
+    ws = align_up(ws + max_ops, kAlign);
     pl.ws_bytes = ws;
     return MTX_OK;
 }
@@ -656,7 +716,7 @@ void glorot_init_host(const Plan& pl, uint64_t seed, std::vector<float>& w)
     for (size_t l = 0; l < pl.L.size(); ++l) {
         const LayerPlan& lp = pl.L[l];
         if (!lp.w_len) continue;
-        if (lp.kind == MTX_BN) {  // gamma = 1, beta = 0: the identity at the start
+        if (lp.kind == MTX_BN || lp.kind == MTX_NORM) {  // gamma = 1, beta = 0
             for (size_t i = 0; i < lp.w_len; ++i) w[lp.w_off + i] = 1.0f;
             continue;
         }
@@ -666,6 +726,9 @@ void glorot_init_host(const Plan& pl, uint64_t seed, std::vector<float>& w)
             fan_out = (double)lp.oc * lp.k * lp.k;
         } else if (lp.kind == MTX_ADDP) {  // a 1x1 convolution of the source's channels
             fan_in = (double)pl.L[lp.src].oc;
+            fan_out = (double)lp.oc;
+        } else if (lp.kind == MTX_EMBED) {
+            fan_in = (double)lp.vocab;
             fan_out = (double)lp.oc;
         } else {
             fan_in = (double)lp.in_elems;
@@ -792,6 +855,12 @@ struct mtx_model {
     float b1 = 0.9f, b2 = 0.999f, eps = 0.0f;
     float* s2 = nullptr;
     long long opt_step = 0;
+    // the embedding's scale and padding token (mtx_set_embedding), clipping (mtx_set_clip_norm)
+    float embed_scale = 1.0f;
+    int embed_pad = -1;
+    float clip_norm = 0.0f;
+    float* clip_out = nullptr;
+    double* clip_ws = nullptr;
     // matrix launches of the last enqueued step (mtx_get_launches)
     std::vector<mtx_launch_info> launches;
     // the workspace is the device's static array (mtx_init_model_static), shared with every
@@ -1079,6 +1148,45 @@ int mtx_set_nonfinite_check(mtx_model* m, int enable)
     return MTX_OK;
 }
 
+int mtx_set_embedding(mtx_model* m, float scale, int pad)
+{
+    if (!m) return fail(MTX_EINVAL, "model is NULL");
+    if (m->pl.L.front().kind != MTX_EMBED) return fail(MTX_EINVAL, "the model has no embedding");
+    if (!std::isfinite(scale)) return fail(MTX_EINVAL, "scale must be finite");
+    m->embed_scale = scale;
+    m->embed_pad = pad;
+    m->graph.reset();  // the captured launch sequence depends on it
+    return MTX_OK;
+}
+
+int mtx_set_clip_norm(mtx_model* m, float max_norm, float* norm_out, void* workspace)
+{
+    if (!m) return fail(MTX_EINVAL, "model is NULL");
+    if (!(max_norm >= 0.0f)) return fail(MTX_EINVAL, "max_norm must be >= 0");
+    if (max_norm > 0.0f) {
+        if (!workspace || !aligned(workspace, 16) || !aligned(norm_out, 4))
+            return fail(MTX_EINVAL, "clipping needs a 16-byte aligned workspace (and a 4-byte "
+                                    "aligned norm_out)");
+        const size_t pb = m->pl.P * 4, gb = m->pl.ld * 4 * m->pl.R;
+        const std::pair<const void*, size_t> mine[] = {{workspace, MTX_CLIP_WORKSPACE_BYTES},
+                                                       {norm_out, norm_out ? 4 : 0}};
+        const std::pair<const void*, size_t> model[] = {{m->w, pb}, {m->v, pb}, {m->grads, gb},
+                                                        {m->gavg, pb}, {m->ws, m->pl.ws_bytes},
+                                                        {m->s2, m->s2 ? pb : 0}};
+        for (const auto& a : mine)
+            for (const auto& b : model)
+                if (a.second && b.second && overlap(a.first, a.second, b.first, b.second))
+                    return fail(MTX_EINVAL, "norm_out or the workspace overlaps a model buffer");
+        if (norm_out && overlap(norm_out, 4, workspace, MTX_CLIP_WORKSPACE_BYTES))
+            return fail(MTX_EINVAL, "norm_out overlaps the workspace");
+    }
+    m->clip_norm = max_norm;
+    m->clip_out = max_norm > 0.0f ? norm_out : nullptr;
+    m->clip_ws = max_norm > 0.0f ? static_cast<double*>(workspace) : nullptr;
+    m->graph.reset();  // the captured launch sequence depends on it
+    return MTX_OK;
+}
+
 int mtx_set_fused_update(mtx_model* m, int enable)
 {
     if (!m) return fail(MTX_EINVAL, "model is NULL");
@@ -1151,19 +1259,25 @@ int mtx_get_timing(mtx_model* m, mtx_kernel_time* out, int capacity, int* count,
 
 // Enqueue the kernels of one step on stream s (eagerly, or into a capture).
 // The average of the R shard gradients of parameters [off, off + len) fused with the model's
-// update rule (Adam at step number m->opt_step, already advanced for this step).
+// update rule (Adam at step number m->opt_step, already advanced for this step); from_avg: the
+// update alone, from grad_avg, unless *skip is set.
 static hipError_t update_slice(mtx_model* m, size_t off, size_t len, float lr, float momentum,
-                               hipStream_t s, unsigned max_blocks)
+                               hipStream_t s, unsigned max_blocks,
+                               bool from_avg = false, const int* skip = nullptr)
 {
     const Plan& pl = m->pl;
+    const float* src = (from_avg ? m->gavg : m->grads) + off;
+    float* avg = from_avg ? nullptr : m->gavg + off;
+    const int R = from_avg ? 1 : pl.R;
+    const size_t ld = from_avg ? align_up(pl.P, 4) : pl.ld;   // (one row: any stride)
     if (m->opt == MTX_OPT_MOMENTUM)
-        return average_update(m->grads + off, pl.R, len, pl.ld, m->w + off, m->v + off, lr,
-                              momentum, m->gavg + off, true, s, max_blocks);
+        return average_update(src, R, len, ld, m->w + off, m->v + off, lr, momentum, avg, true, s,
+                              max_blocks, skip);
     AdaptParams p;
     p.w = m->w + off;
     p.s1 = m->v + off;
     p.s2 = m->opt == MTX_OPT_ADAM ? m->s2 + off : nullptr;
-    p.avg = m->gavg + off;
+    p.avg = avg;
     p.lr = lr;
     p.eps = m->eps;
     p.b1 = p.c1 = p.b2 = p.c2 = p.ib1 = p.ib2 = 0.0f;
@@ -1176,7 +1290,7 @@ static hipError_t update_slice(mtx_model* m, size_t off, size_t len, float lr, f
         p.ib1 = (float)(1.0 / (1.0 - std::pow((double)m->b1, t)));
         p.ib2 = (float)(1.0 / (1.0 - std::pow((double)m->b2, t)));
     }
-    return average_adapt(m->grads + off, pl.R, len, pl.ld, m->opt == MTX_OPT_ADAM, p, s,
+    return average_adapt(src, R, len, ld, m->opt == MTX_OPT_ADAM, p, s,
                          max_blocks);
 }
 
@@ -1304,6 +1418,31 @@ static int enqueue_step(mtx_model* m, const float* x, const int32_t* labels, flo
                                       other, with_add ? ws + ap->act_off : nullptr,
                                       with_add && ap->relu);
                     }), "batch norm forward");
+        } else if (lp.kind == MTX_EMBED) {
+            HIP_TRY(launch_site(m, "embed_fwd", (int)l, s, [&] {
+                        return embed_fwd(m->w + lp.w_off, DT_F32, lp.vocab, lp.oc,
+                                         reinterpret_cast<const int*>(x),
+                                         (long long)pl.B * lp.h * lp.w, m->embed_pad,
+                                         m->embed_scale, out, dt, lp.oc, s);
+                    }), "embedding");
+        } else if (lp.kind == MTX_NORM) {
+            if (!add_done[l])
+                HIP_TRY(launch_site(m, "norm_fwd", (int)l, s, [&] {
+                            return block_norm_fwd(norm_args(lp, pl.dt, pl.B, m->w + lp.w_off, bias),
+                                                  in, nullptr, nullptr, out,
+                                                  reinterpret_cast<float*>(ws + lp.stat_off), s);
+                        }), "norm forward");
+        } else if (lp.kind == MTX_ADD && !add_done[l] && !lp.relu && l + 1 < pl.L.size() &&
+                   pl.L[l + 1].kind == MTX_NORM) {
+            // the addition and the norm after it in one pass
+            const LayerPlan& np = pl.L[l + 1];
+            add_done[l + 1] = 1;
+            HIP_TRY(launch_site(m, "norm_fwd", (int)l + 1, s, [&] {
+                        return block_norm_fwd(norm_args(np, pl.dt, pl.B, m->w + np.w_off,
+                                                        m->w + np.b_off),
+                                              ws + pl.L[lp.src].act_off, in, out, ws + np.act_off,
+                                              reinterpret_cast<float*>(ws + np.stat_off), s);
+                    }), "residual addition + norm forward");
         } else if (lp.kind == MTX_ADD) {
             if (!add_done[l])
                 HIP_TRY(launch_site(m, "add_fwd", (int)l, s, [&] {
@@ -1346,7 +1485,8 @@ static int enqueue_step(mtx_model* m, const float* x, const int32_t* labels, flo
     // output gradient and input, so (unless kernels are being timed) it runs on the second
     // stream, forked after its output gradient is written and joined before the update.
     const bool overlap = m->overlap && !m->timer.on;
-    const bool layerwise = m->layerwise && m->upd && !m->timer.on && !m->check_finite;
+    const bool clip = m->clip_norm > 0.0f;
+    const bool layerwise = m->layerwise && m->upd && !m->timer.on && !m->check_finite && !clip;
     float* partial_w = overlap ? reinterpret_cast<float*>(ws + pl.partial_w_off) : partial;
     const long long ld = (long long)pl.ld;
     int nfork = 0, nlayer = 0;
@@ -1360,7 +1500,7 @@ static int enqueue_step(mtx_model* m, const float* x, const int32_t* labels, flo
     std::vector<std::pair<size_t, size_t>> rest;
     {
         const bool can = m->fuse_update && m->opt == MTX_OPT_MOMENTUM && !layerwise &&
-                         !m->check_finite;
+                         !m->check_finite && !clip;
         size_t beg = 0;
         for (size_t l = 0; l < pl.L.size(); ++l) {
             const LayerPlan& lp = pl.L[l];
@@ -1383,7 +1523,8 @@ static int enqueue_step(mtx_model* m, const float* x, const int32_t* labels, flo
         // The first parameter layer has no data gradient to run beside: its weight gradient runs
         // on the caller's stream, beside the weight gradients still running on the second stream
         // (measured on the AlexNet step: conv1's weight gradient no longer trails the others).
-        const bool side = lp.w_len && overlap && lp.kind != MTX_BN && l != pl.first_param;
+        const bool side = lp.w_len && overlap && lp.kind != MTX_BN && lp.kind != MTX_NORM &&
+                          l != pl.first_param;
         float* part_wg = side ? partial_w : partial;
         if (side) {
             HIP_TRY(hipEventRecord(m->fork[nfork], s), "fork");
@@ -1474,6 +1615,28 @@ static int enqueue_step(mtx_model* m, const float* x, const int32_t* labels, flo
                                       reinterpret_cast<float*>(ws + pl.bn_coef_off), m->grads, ld,
                                       (long long)lp.w_off, (long long)lp.b_off, s);
                     }), "batch norm backward");
+        } else if (lp.kind == MTX_EMBED) {
+            HIP_TRY(launch_site(m, "embed_bwd", l, s, [&] {
+                        return embed_bwd(reinterpret_cast<const int*>(x),
+                                         (long long)pl.Nb * lp.h * lp.w, pl.R, dy, dt, lp.oc,
+                                         lp.vocab, lp.oc, m->embed_pad, m->embed_scale,
+                                         m->grads + lp.w_off, ld, false, ws + pl.ops_off, s);
+                    }), "embedding gradient");
+        } else if (lp.kind == MTX_NORM) {
+            BlockNormGrads g{};
+            g.h_out = in_l;
+            g.stats = reinterpret_cast<const float*>(ws + lp.stat_off);
+            g.dy = dy;
+            g.dh = dx;
+            g.pre_w = m->grads + lp.w_off;
+            g.pre_b = lp.b_len ? m->grads + lp.b_off : nullptr;
+            g.ld = ld;
+            g.relu_h = mask != nullptr;   // (its input is that layer's output)
+            HIP_TRY(launch_site(m, "norm_bwd", l, s, [&] {
+                        return block_norm_bwd(norm_args(lp, pl.dt, pl.B, m->w + lp.w_off,
+                                                        m->w + lp.b_off), pl.R, g,
+                                              ws + pl.ops_off, s);
+                    }), "norm backward");
         } else if (lp.kind == MTX_ADD) {
             // the previous layer's share: dy (times its ReLU mask), unless it reads dy itself;
             // the source's share is added from dy when the source's gradient is written
@@ -1575,6 +1738,18 @@ static int enqueue_step(mtx_model* m, const float* x, const int32_t* labels, flo
         return MTX_OK;
     }
     // ---- average of the R shard gradients fused with the optimizer step ----
+    if (clip) {
+        // the average, added as the update rule adds it, with its norm; clipped; then the update
+        int* flag = m->check_finite ? reinterpret_cast<int*>(ws + pl.sync_off + 64) : nullptr;
+        HIP_TRY(launch_site(m, "avg_clip", -1, s, [&] {
+                    return average_clip(m->grads, pl.R, pl.P, pl.ld, m->opt != MTX_OPT_MOMENTUM,
+                                        m->clip_norm, m->gavg, m->clip_out, flag, m->clip_ws, s);
+                }), "average + clip");
+        HIP_TRY(launch_site(m, "avg_update", -1, s, [&] {
+                    return update_slice(m, 0, pl.P, lr, momentum, s, 0, true, flag);
+                }), "update");
+        return MTX_OK;
+    }
     if (m->check_finite) {
         // the average first, with a flag for a non-finite value; then the momentum update from
         // the stored average (g = avg / 1: the same values as the fused pass), which does
@@ -1637,13 +1812,17 @@ static bool capture_step(mtx_model* m, const float* x, const int32_t* labels, fl
 static int step_dispatch(mtx_model* m, const float* x, const int32_t* labels, float lr,
                          float momentum, float* loss_out, hipStream_t s, bool caller_capturing);
 
-int mtx_train_step(mtx_model* m, const float* x, const int32_t* labels, float lr,
-                   float momentum, float* loss_out, void* stream)
+// mtx_train_step, or mtx_train_step_tokens with the tokens at x.
+static int train_step(mtx_model* m, const float* x, bool tokens, const int32_t* labels, float lr,
+                      float momentum, float* loss_out, void* stream)
 {
     if (!m) return fail(MTX_EINVAL, "model is NULL");
     if (!x || !labels) return fail(MTX_EINVAL, "x and labels must not be NULL");
-    if (!aligned(x, 16) || !aligned(labels, 4) || (loss_out && !aligned(loss_out, 4)))
-        return fail(MTX_EINVAL, "x must be 16-byte aligned, labels and loss_out 4-byte aligned");
+    if (tokens != (m->pl.L.front().kind == MTX_EMBED))
+        return fail(MTX_EINVAL, tokens ? "the network's first layer is not MTX_EMBED: use mtx_train_step"
+                                       : "the network's first layer is MTX_EMBED: use mtx_train_step_tokens");
+    if (!aligned(x, tokens ? 4 : 16) || !aligned(labels, 4) || (loss_out && !aligned(loss_out, 4)))
+        return fail(MTX_EINVAL, "x must be 16-byte aligned; tokens, labels and loss_out 4-byte aligned");
     if (!std::isfinite(lr) || !std::isfinite(momentum))
         return fail(MTX_EINVAL, "lr and momentum must be finite");
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -1668,6 +1847,19 @@ int mtx_train_step(mtx_model* m, const float* x, const int32_t* labels, float lr
         return MTX_OK;
     }
     return step_dispatch(m, x, labels, lr, momentum, loss_out, s, caller_capturing);
+}
+
+int mtx_train_step(mtx_model* m, const float* x, const int32_t* labels, float lr, float momentum,
+                   float* loss_out, void* stream)
+{
+    return train_step(m, x, false, labels, lr, momentum, loss_out, stream);
+}
+
+int mtx_train_step_tokens(mtx_model* m, const int32_t* tokens, const int32_t* labels, float lr,
+                          float momentum, float* loss_out, void* stream)
+{
+    return train_step(m, reinterpret_cast<const float*>(tokens), true, labels, lr, momentum,
+                      loss_out, stream);
 }
 
 // The step on stream s: replayed from the model's graph, captured into it, or enqueued directly.
@@ -1717,7 +1909,9 @@ int mtx_set_optimizer(mtx_model* m, int kind, float beta1, float beta2, float ep
             return fail(MTX_EINVAL, "Adam needs a 16-byte aligned second-moment buffer");
         const size_t nb = m->pl.P * 4;
         if (overlap(s2, nb, m->w, nb) || overlap(s2, nb, m->v, nb) ||
-            overlap(s2, nb, m->gavg, nb) || overlap(s2, nb, m->grads, m->pl.ld * m->pl.R * 4))
+            overlap(s2, nb, m->gavg, nb) || overlap(s2, nb, m->grads, m->pl.ld * m->pl.R * 4) ||
+            (m->clip_ws && overlap(s2, nb, m->clip_ws, MTX_CLIP_WORKSPACE_BYTES)) ||
+            (m->clip_out && overlap(s2, nb, m->clip_out, 4)))
             return fail(MTX_EINVAL, "the second-moment buffer overlaps the model's buffers");
     }
     m->opt = kind;

@@ -551,6 +551,7 @@ hipError_t block_norm_bwd(const BlockNorm& b, int R, const BlockNormGrads& g, vo
     if (!g.pre_w && !g.post_w && !g.gate && !g.pre_b && !g.post_b) return hipSuccess;
     const long long rows = (long long)R * kPlanes +
                            (group_gate && g.gate && q.pieces > 1 ? q.groups_shard * R : 0);
+    if (q.blocks) timing_split(s, "join");
     hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)rows, (b.D + 255) / 256), dim3(1024), 0, s, g,
                        q, R, b.D, group_gate, part);
     return hipGetLastError();

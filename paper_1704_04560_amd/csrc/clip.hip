@@ -198,6 +198,7 @@ hipError_t average_clip(const float* grads, int R, size_t n, size_t ld, bool exa
     else launch_avg_sq<false>(grads, R, n, ld, avg, part, blocks, vec, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
+    timing_split(s, "scale");
     const ClipOut o{max_norm, norm_out, nonfinite};
     const unsigned sblocks = (unsigned)std::min<size_t>(kClipBlocks, (n + 1023) / 1024);
     if (vec_avg)

@@ -644,6 +644,7 @@ static hipError_t launch_gather(EmbedGather a, hipStream_t s)
                        dim3(kGatherThreads), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.pieces <= 1) return e;
+    timing_split(s, "join");
     const long long js = (a.D + kJoinCols - 1) / kJoinCols;
     hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(pieces * js)), dim3(256), 0, s, a);
     return hipGetLastError();
@@ -704,6 +705,7 @@ hipError_t embed_bwd(const int* tok, long long n, int R, const void* dy, Dt dt, 
     hipLaunchKernelGGL(embed_index_kernel, grid, block, lds, s, x);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
+    timing_split(s, "gather");
     return dt == DT_F32 ? launch_gather<float>(a, vec, s) : launch_gather<bf16_t>(a, vec, s);
 }
 

@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(HERE, "libmtx.so")
 MTX_OK, MTX_EINVAL, MTX_ENOMEM, MTX_EHIP, MTX_EUNSUPPORTED, MTX_ENONFINITE = 0, -1, -2, -3, -4, -5
 MTX_F32, MTX_BF16 = 0, 1
 MTX_FC, MTX_CONV, MTX_MAXPOOL, MTX_BN, MTX_ADD, MTX_ADDP = 0, 1, 2, 3, 4, 5
+MTX_EMBED, MTX_NORM = 6, 7
 MTX_OPT_MOMENTUM, MTX_OPT_ADAM, MTX_OPT_ADAGRAD = 0, 1, 2
 MTX_NORM_RMS, MTX_NORM_LAYER = 0, 1
 MTX_CLIP_WORKSPACE_BYTES = 32768
@@ -33,7 +34,7 @@ EXPORTS = ("mtx_model_sizes", "mtx_init_model", "mtx_init_model_static", "mtx_tr
            "mtx_embed_forward", "mtx_embed_sizes", "mtx_embed_backward",
            "mtx_block_norm_forward", "mtx_block_norm_sizes", "mtx_block_norm_backward",
            "mtx_average_clip", "mtx_clip_sizes", "mtx_init_clip", "mtx_clip_grads",
-           "mtx_free_clip")
+           "mtx_free_clip", "mtx_train_step_tokens", "mtx_set_embedding", "mtx_set_clip_norm")
 
 
 class MtxError(RuntimeError):
@@ -127,6 +128,9 @@ def lib() -> C.CDLL:
             "mtx_get_launches": (i32, [vp, C.POINTER(mtx_launch_info), i32, C.POINTER(i32)]),
             "mtx_free_model": (None, [vp]),
             "mtx_last_error": (C.c_char_p, []),
+            "mtx_train_step_tokens": (i32, [vp, vp, vp, f32, f32, vp, vp]),
+            "mtx_set_embedding": (i32, [vp, f32, i32]),
+            "mtx_set_clip_norm": (i32, [vp, f32, vp, vp]),
             "mtx_embed_forward": (i32, [vp, i32, i32, i32, vp, sz, i32, f32, vp, i32, sz, vp]),
             "mtx_embed_sizes": (i32, [sz, i32, i32, i32, C.POINTER(sz)]),
             "mtx_embed_backward": (i32, [vp, sz, i32, vp, i32, sz, i32, i32, i32, f32, vp, sz,
@@ -213,6 +217,19 @@ def mtx_init_model_static(desc, R, shard_batch, seed, w, v, grads, grad_avg, str
 def mtx_train_step(handle, x, labels, lr, momentum, loss_out=None, stream=None):
     _check(lib().mtx_train_step(handle, _ptr(x), _ptr(labels), lr, momentum, _ptr(loss_out),
                                 _stream(stream)))
+
+
+def mtx_train_step_tokens(handle, tokens, labels, lr, momentum, loss_out=None, stream=None):
+    _check(lib().mtx_train_step_tokens(handle, _ptr(tokens), _ptr(labels), lr, momentum,
+                                       _ptr(loss_out), _stream(stream)))
+
+
+def mtx_set_embedding(handle, scale=1.0, pad=-1):
+    _check(lib().mtx_set_embedding(handle, scale, pad))
+
+
+def mtx_set_clip_norm(handle, max_norm, norm_out=None, workspace=None):
+    _check(lib().mtx_set_clip_norm(handle, max_norm, _ptr(norm_out), _ptr(workspace)))
 
 
 def mtx_average_grads(grads, R, n, ld, avg, stream=None):
@@ -465,11 +482,13 @@ class Model:
         c, h, w = self.in_shape
         out = []
         for (kind, o, k, s, p, g, relu) in self.layers:
-            if kind == MTX_CONV:
+            if kind == MTX_EMBED:
+                c = o
+            elif kind == MTX_CONV:
                 c, h, w = o, (h + 2 * p - k) // s + 1, (w + 2 * p - k) // s + 1
             elif kind == MTX_FC:
                 c, h, w = o, 1, 1
-            elif kind in (MTX_BN, MTX_ADD, MTX_ADDP):
+            elif kind in (MTX_BN, MTX_ADD, MTX_ADDP, MTX_NORM):
                 pass
             else:
                 h, w = (h - k) // s + 1, (w - k) // s + 1
@@ -477,7 +496,19 @@ class Model:
         return out
 
     def train_step(self, x, labels, lr, momentum, loss_out=None, stream=None):
-        mtx_train_step(self.handle, x, labels, lr, momentum, loss_out, stream)
+        """x: images, or the tokens (int32) of a network that begins with MTX_EMBED."""
+        step = mtx_train_step_tokens if self.layers[0][0] == MTX_EMBED else mtx_train_step
+        step(self.handle, x, labels, lr, momentum, loss_out, stream)
+
+    def set_clip_norm(self, max_norm, norm_out=None):
+        """Clip the averaged gradient's global norm in train_step (0: off); norm_out: a device
+        float32 [1] that receives the norm of every step."""
+        import torch
+        ws = None
+        if max_norm > 0:
+            ws = torch.empty(MTX_CLIP_WORKSPACE_BYTES, dtype=torch.uint8, device=self.w.device)
+        mtx_set_clip_norm(self.handle, max_norm, norm_out, ws)
+        self._clip = (norm_out, ws)
 
     def set_optimizer(self, kind, beta1=0.9, beta2=0.999, eps=1e-8):
         """Select the update rule of train_step; Adam gets a zeroed second-moment buffer."""

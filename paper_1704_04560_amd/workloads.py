@@ -28,7 +28,7 @@ from typing import List, Tuple
 
 import numpy as np
 
-FC, CONV, MAXPOOL, BN, ADD, ADDP = 0, 1, 2, 3, 4, 5
+FC, CONV, MAXPOOL, BN, ADD, ADDP, EMBED, NORM = 0, 1, 2, 3, 4, 5, 6, 7
 F32, BF16 = 0, 1
 
 STREAM_X, STREAM_LABELS, STREAM_W, STREAM_V, STREAM_G, STREAM_S2 = 0, 1, 2, 3, 4, 5
@@ -72,6 +72,16 @@ def addp(src, out, stride=1, relu=False):
     convolution of the given stride (out = this layer's channel count, with weights and bias)
     and is added to the previous layer's output (ResNet-50's downsampling blocks)."""
     return Layer(ADDP, out, src, stride, 0, 1, relu)
+
+
+def embed(tokens, out):
+    """Token embedding, the first layer: a table of `tokens` rows of `out` values."""
+    return Layer(EMBED, out, tokens, 1, 0, 1, False)
+
+
+def norm(layer=True):
+    """Norm of each position over its channels: layer norm, or RMS norm."""
+    return Layer(NORM, 0, 1 if layer else 0, 1, 0, 1, False)
 
 
 @dataclass(frozen=True)

@@ -175,3 +175,34 @@ def test_python_lists_of_tensors():
     arr = mtx.make_tensor_list([(t, t), (torch.zeros(3, dtype=torch.bfloat16), torch.zeros(3))])
     assert arr[0].src == arr[0].dst and arr[1].src_type == B and arr[1].dst_type == F
     assert np.int64(arr[1].n) == 3
+
+
+def test_token_networks():
+    from paper_1704_04560_amd import workloads as wl
+
+    def code_of(layers, shape=(1, 4, 1), dt=F, R=2):
+        t = [(l.kind, l.out, l.k, l.stride, l.pad, l.groups, int(l.relu)) if isinstance(l, wl.Layer)
+             else l for l in layers]
+        with pytest.raises(mtx.MtxError) as e:
+            mtx.mtx_model_sizes(mtx.make_desc(shape, t, dt), R, 2)
+        return e.value.code
+
+    ok = [wl.embed(10, 8), wl.norm(), wl.fc(3)]
+    d = mtx.make_desc((1, 4, 1), [(l.kind, l.out, l.k, l.stride, l.pad, l.groups, 0) for l in ok], F)
+    P, ld, ws = mtx.mtx_model_sizes(d, 2, 2)
+    assert P == 10 * 8 + 2 * 8 + 3 * 32 + 3 and ld >= P and ws > 0
+    for bad in ([wl.norm(), wl.embed(10, 8), wl.fc(3)], [wl.embed(0, 8), wl.fc(3)],
+                [wl.embed(10, 0), wl.fc(3)], [(6, 8, 10, 1, 1, 1, 0), wl.fc(3)],
+                [(6, 8, 10, 1, 0, 1, 1), wl.fc(3)], [(6, 8, 10, 2, 0, 1, 0), wl.fc(3)],
+                [(6, 8, 10, 1, 0, 2, 0), wl.fc(3)], [wl.embed(10, 8), (7, 9, 0, 1, 0, 1, 0), wl.fc(3)],
+                [wl.embed(10, 8), (7, 0, 2, 1, 0, 1, 0), wl.fc(3)],
+                [wl.embed(10, 8), (7, 0, 1, 1, 0, 1, 1), wl.fc(3)],
+                [wl.embed(10, 8), (7, 0, 1, 1, 2, 1, 0), wl.fc(3)], [wl.embed(10, 8), wl.norm()]):
+        assert code_of(bad) == mtx.MTX_EINVAL, bad
+    assert code_of(ok, shape=(2, 4, 1)) == mtx.MTX_EINVAL
+    assert code_of(ok, R=65537) == mtx.MTX_EINVAL
+    assert code_of([wl.embed(10, 16385), wl.norm(), wl.fc(3)]) == mtx.MTX_EUNSUPPORTED
+    for f in (lambda: mtx.mtx_train_step_tokens(None, A[0], A[1], 0.1, 0.0, stream=0),
+              lambda: mtx.mtx_set_embedding(None), lambda: mtx.mtx_set_clip_norm(None, 1.0)):
+        with pytest.raises(mtx.MtxError):
+            f()
