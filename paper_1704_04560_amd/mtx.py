@@ -169,10 +169,19 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+_raw_stream = None   # (): the current stream's handle
+
+
 def _stream(stream) -> Optional[int]:
+    global _raw_stream
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream or None
+        if _raw_stream is None:
+            import torch
+            get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            # (a Stream object costs more host time than a small kernel takes)
+            _raw_stream = ((lambda: get(torch.cuda.current_device())) if get else
+                           (lambda: torch.cuda.current_stream().cuda_stream))
+        return _raw_stream() or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
