@@ -19,6 +19,7 @@
 
 namespace mtx {
 
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 // A thread's N = W C elements.  AL (rows of a multiple of W elements, aligned): runs of W, element k at
@@ -29,35 +30,51 @@ template <int NT, int W, bool AL> __device__ __forceinline__ int elem(int l, int
     return AL ? ((k / W) * NT + l) * W + k % W : k * NT + l;
 }
 
-template <int BYTES> struct Vec { typedef u32x4 type; };
-template <> struct Vec<8> { typedef unsigned type __attribute__((ext_vector_type(2))); };
-
 // N elements as they are stored: 32-bit words (AL), or one by one.
 template <typename T, int N, bool AL> struct Raw {
     unsigned w[AL ? N * (int)sizeof(T) / 4 : 1];
     T e[AL ? 1 : N];
 };
 
+// A row as a buffer of D elements: what lies past its end reads as zero and is not written, without a
+// branch or a mask for it (8850 rows of 771 fp32, backward: 53 -> 47 us).  The pointer is the same
+// in every lane of a wave.
+template <typename T> __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const T* p, int D)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p), 0, D * (int)sizeof(T), 0x00020000);
+}
+
 template <typename T, int NT, int W, int C, bool AL>
 __device__ __forceinline__ void load_raw(const T* p, int l, int D, Raw<T, W * C, AL>& o)
 {
+    const __amdgpu_buffer_rsrc_t r = row_buffer(p, D);
     if constexpr (AL) {
-        typedef typename Vec<W * (int)sizeof(T)>::type V;
-        constexpr int words = sizeof(V) / 4, per = W * (int)sizeof(T) / (int)sizeof(V);
+        constexpr int bytes = W * (int)sizeof(T);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int d = (c * NT + l) * W;
+            const int at = (c * NT + l) * bytes;
+            if constexpr (bytes == 8) {
+                const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0);
+                o.w[2 * c] = v[0];
+                o.w[2 * c + 1] = v[1];
+            } else {
 #pragma unroll
-            for (int q = 0; q < per; ++q) {
-                V v{};
-                if (d < D) v = reinterpret_cast<const V*>(p + d)[q];
+                for (int q = 0; q < bytes / 16; ++q) {
+                    const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(r, at + 16 * q, 0, 0);
 #pragma unroll
-                for (int j = 0; j < words; ++j) o.w[(c * per + q) * words + j] = v[j];
+                    for (int j = 0; j < 4; ++j) o.w[(c * (bytes / 16) + q) * 4 + j] = v[j];
+                }
             }
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < W * C; ++k) o.e[k] = k * NT + l < D ? p[k * NT + l] : T(0);
+        for (int k = 0; k < W * C; ++k) {
+            const int at = (k * NT + l) * (int)sizeof(T);
+            if constexpr (sizeof(T) == 4)
+                o.e[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0));
+            else
+                o.e[k] = __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0);
+        }
     }
 }
 
@@ -72,27 +89,38 @@ __device__ __forceinline__ float raw_at(const Raw<T, N, AL>& o, int k)
 template <typename T, int NT, int W, int C, bool AL>
 __device__ __forceinline__ void store_row(T* p, int l, int D, const float (&v)[W * C])
 {
+    const __amdgpu_buffer_rsrc_t r = row_buffer(p, D);
     if constexpr (AL) {
-        typedef typename Vec<W * (int)sizeof(T)>::type V;
-        constexpr int per = W * (int)sizeof(T) / (int)sizeof(V);
+        constexpr int bytes = W * (int)sizeof(T);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int d = (c * NT + l) * W;
-            if (d >= D) continue;
+            const int at = (c * NT + l) * bytes;
             T e[W];
 #pragma unroll
             for (int k = 0; k < W; ++k) e[k] = from_f32<T>(v[W * c + k]);
+            if constexpr (bytes == 8) {
+                u32x2 raw;
+                __builtin_memcpy(&raw, e, 8);
+                __builtin_amdgcn_raw_buffer_store_b64(raw, r, at, 0, 0);
+            } else {
 #pragma unroll
-            for (int q = 0; q < per; ++q) {
-                V raw;
-                __builtin_memcpy(&raw, e + q * W / per, sizeof(V));
-                reinterpret_cast<V*>(p + d)[q] = raw;
+                for (int q = 0; q < bytes / 16; ++q) {
+                    u32x4 raw;
+                    __builtin_memcpy(&raw, e + q * 16 / (int)sizeof(T), 16);
+                    __builtin_amdgcn_raw_buffer_store_b128(raw, r, at + 16 * q, 0, 0);
+                }
             }
         }
     } else {
 #pragma unroll
-        for (int k = 0; k < W * C; ++k)
-            if (k * NT + l < D) p[k * NT + l] = from_f32<T>(v[k]);
+        for (int k = 0; k < W * C; ++k) {
+            const int at = (k * NT + l) * (int)sizeof(T);
+            const T e = from_f32<T>(v[k]);
+            if constexpr (sizeof(T) == 4)
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, e), r, at, 0, 0);
+            else
+                __builtin_amdgcn_raw_buffer_store_b16(e, r, at, 0, 0);
+        }
     }
 }
 
@@ -133,7 +161,8 @@ __global__ __launch_bounds__(block_of(NT)) void norm_fwd_kernel(BlockNorm b, con
     const int l = threadIdx.x % NT, D = b.D;
     const float inv_d = 1.0f / (float)D;
     // (a block's rows run together: those past the end repeat the last one, storing nothing)
-    const long long want = (long long)blockIdx.x * RPB + threadIdx.x / NT;
+    const long long want = (long long)blockIdx.x * RPB +
+                           __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
     const bool live = want < b.rows;
     const long long i = live ? want : b.rows - 1;
     Raw<T, N, AL> rh, rx;
@@ -299,7 +328,14 @@ static NormDeal norm_deal(const BlockNorm& b, int R, bool al)
 // planes of a block's partial sums
 enum { PL_PRE_W, PL_POST_W, PL_GATE, PL_PRE_B, PL_POST_B, kPlanes };
 
-template <typename T, int W, int NT, int C, bool AL, bool LAYER>
+// Within a group du = scale gate dH with one gate vector, so the sums over its rows come from two:
+//   t1 = sum dH x^ (x where there is no post norm),  t0 = sum dH:
+//   d_post_w = scale gate t1, d_post_b = scale gate t0, d_gate = scale (post_w t1 + post_b t0).
+// MANY: a block of several whole groups adds d_post_w and d_post_b over them.  The next row's dy and
+// h_out are loaded while a row is worked on; dh_out and x arrive during its first sum (8850 x 771:
+// 47 -> 44 us).  8192 x 4096 bf16, four shards: 97 us, 4.4 TB/s with the partial sums; half the
+// blocks 128, twice as many 100.
+template <typename T, int W, int NT, int C, bool AL, bool LAYER, bool MANY>
 __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(BlockNorm b, BlockNormGrads g,
                                                                 NormDeal q, float* __restrict__ part)
 {
@@ -307,28 +343,26 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
     __shared__ float red[2][M][16];
     __shared__ float comb[RPB > 1 ? RPB - 1 : 1][RPB > 1 ? N * NT : 1];
     int slot = 0;
-    const int l = threadIdx.x % NT, rs = threadIdx.x / NT, D = b.D;
+    const int l = threadIdx.x % NT, D = b.D;
+    const int rs = __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
     const float inv_d = 1.0f / (float)D;
     const long long shard = blockIdx.x / q.blocks_shard, bs = blockIdx.x % q.blocks_shard;
     const long long nb = q.group * q.groups_shard;
-    long long g0, g1;   // the block's groups, within the shard
-    int first = 0;      // its first row within the group
-    if (q.pieces > 1) {
-        g0 = bs / q.pieces;
-        g1 = g0 + 1;
-        first = (int)(bs % q.pieces) * q.chunk;
-    } else {
-        g0 = bs * q.gpb;
-        g1 = min(g0 + q.gpb, q.groups_shard);
-    }
-    const int rows = (int)max(0LL, min((long long)q.chunk, q.group - first));   // of each group
+    // the block's groups, and its rows within each (runs of rows; interleaved ones took the same time)
+    const long long g0 = MANY ? bs * q.gpb : bs / q.pieces;
+    const long long g1 = MANY ? min(g0 + q.gpb, q.groups_shard) : g0 + 1;
+    const int first = MANY ? 0 : (int)(bs % q.pieces) * q.chunk;
+    const int rows = (int)max(0LL, min((long long)q.chunk, q.group - first));
     const bool has_x = g.x != nullptr, has_y = g.dy != nullptr;
     const bool post = b.post_w != nullptr;
-    float pw[N], qw[N], gt[N], pb[LAYER ? N : 1], qb[LAYER ? N : 1];
+    float pw[N], t1[N], pb[LAYER ? N : 1], t0[LAYER ? N : 1];
+    float qw[MANY ? N : 1], qb[MANY && LAYER ? N : 1];
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        pw[k] = qw[k] = gt[k] = 0.f;
-        if (LAYER) pb[k] = qb[k] = 0.f;
+        pw[k] = t1[k] = 0.f;
+        if (LAYER) pb[k] = t0[k] = 0.f;
+        if (MANY) qw[k] = 0.f;
+        if (MANY && LAYER) qb[k] = 0.f;
     }
     // add the row slots' sums in order, into the first one's
     auto combine = [&](float (&v)[N]) {
@@ -345,26 +379,33 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
                     for (int k = 0; k < N; ++k) v[k] += comb[o][k * NT + l];
         }
     };
+    float* out = part + (long long)blockIdx.x * kPlanes * q.Dp;
+    auto put = [&](int plane, const float (&v)[N]) {
+        if (rs == 0) store_row<float, NT, W, C, AL>(out + (long long)plane * q.Dp, l, D, v);
+    };
+    auto row_of = [&](long long gi, int j0) {
+        return shard * nb + gi * q.group + first + (j0 + rs < rows ? j0 + rs : 0);
+    };
+    Raw<T, N, AL> rH, ry;
+    auto load_y = [&](long long i) {
+        load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.dy) + i * b.ld_y, l, D, ry);
+        load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.h_out) + i * b.ld_h, l, D, rH);
+    };
+    if (has_y && rows && g0 < g1) load_y(row_of(g0, 0));
     for (long long gi = g0; gi < g1; ++gi) {
-        const long long base = shard * nb + gi * q.group + first;
+        const long long base = shard * nb + gi * q.group;
         const float* gate = b.gate ? b.gate + (b.gate_rows ? base / b.gate_rows : 0) * D : nullptr;
         for (int j0 = 0; j0 < rows; j0 += RPB) {
             const bool live = j0 + rs < rows;
-            const long long i = base + (live ? j0 + rs : 0);
-            Raw<T, N, AL> rH, ry, ro, rx;
+            const long long i = row_of(gi, j0);
+            Raw<T, N, AL> ro, rx;
             Raw<float, N, AL> rw;
             float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
             if (g.stats) st = *reinterpret_cast<const float4*>(g.stats + 4 * i);
-            float dH[N];
-            if (has_y) {
-                load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.h_out) + i * b.ld_h, l, D, rH);
-                load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.dy) + i * b.ld_y, l, D, ry);
-            }
             if (g.dh_out)
                 load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.dh_out) + i * b.ld_h, l, D, ro);
             if (has_x) load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.x) + i * b.ld_x, l, D, rx);
-#pragma unroll
-            for (int k = 0; k < N; ++k) dH[k] = g.dh_out ? raw_at(ro, k) : 0.f;
+            float dH[N];
             if (has_y) {
                 load_raw<float, NT, W, C, AL>(b.pre_w, l, D, rw);
                 float s[M] = {};
@@ -379,12 +420,16 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
 #pragma unroll
                 for (int k = 0; k < N; ++k) {
                     const float dy = raw_at(ry, k), hat = (raw_at(rH, k) - st.z) * st.w;
-                    dH[k] += st.w * (dy * raw_at(rw, k) - c0 - hat * c1);
+                    dH[k] = (g.dh_out ? raw_at(ro, k) : 0.f) +
+                            st.w * (dy * raw_at(rw, k) - c0 - hat * c1);
                     if (live) {
                         pw[k] = fmaf(dy, hat, pw[k]);
                         if (LAYER) pb[k] += dy;
                     }
                 }
+            } else {
+#pragma unroll
+                for (int k = 0; k < N; ++k) dH[k] = raw_at(ro, k);
             }
             if (g.dh && live) {
                 if (g.relu_h) {
@@ -396,71 +441,112 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
                     store_row<T, NT, W, C, AL>(static_cast<T*>(g.dh) + i * b.ld_h, l, D, dH);
                 }
             }
+            if (has_y) {
+                if (j0 + RPB < rows) load_y(row_of(gi, j0 + RPB));
+                else if (MANY && gi + 1 < g1) load_y(row_of(gi + 1, 0));
+            }
             if (!has_x) continue;
-            // du = scale gate dH; the gate's gradient is scale sum dH u
-            float du[N];
+            if (live) {
+                // (past D, dH is not 0; its sums there are not stored)
+                const float m = post ? st.x : 0.f, r = post ? st.y : 1.f;
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    t1[k] = fmaf(dH[k], (raw_at(rx, k) - m) * r, t1[k]);
+                    if (LAYER) t0[k] += dH[k];
+                }
+            }
+            if (!g.dx) continue;   // (the same in every thread)
+            // dH becomes du = scale gate dH, then dx
             if (gate) {
                 Raw<float, N, AL> rg;
                 load_raw<float, NT, W, C, AL>(gate, l, D, rg);
 #pragma unroll
-                for (int k = 0; k < N; ++k) du[k] = b.scale * raw_at(rg, k) * dH[k];
+                for (int k = 0; k < N; ++k) dH[k] *= b.scale * raw_at(rg, k);
             } else {
 #pragma unroll
-                for (int k = 0; k < N; ++k) du[k] = b.scale * dH[k];
+                for (int k = 0; k < N; ++k) dH[k] *= b.scale;
             }
-            if (!post) {
-                if (live)
+            if (post) {
+                load_raw<float, NT, W, C, AL>(b.post_w, l, D, rw);
+                float s[M] = {};
 #pragma unroll
-                    for (int k = 0; k < N; ++k) gt[k] = fmaf(b.scale * dH[k], raw_at(rx, k), gt[k]);
-                if (g.dx && live) store_row<T, NT, W, C, AL>(static_cast<T*>(g.dx) + i * b.ld_x, l, D, du);
-                continue;
+                for (int k = 0; k < N; ++k) {
+                    dH[k] *= raw_at(rw, k);   // (0 past D)
+                    s[0] = fmaf(dH[k], (raw_at(rx, k) - st.x) * st.y, s[0]);
+                    if (LAYER) s[M - 1] += dH[k];
+                }
+                row_sum<NT, M>(s, red, slot);
+                const float c1 = s[0] * inv_d, c0 = LAYER ? s[M - 1] * inv_d : 0.f;
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    dH[k] = st.y * (dH[k] - c0 - (raw_at(rx, k) - st.x) * st.y * c1);
             }
-            load_raw<float, NT, W, C, AL>(b.post_w, l, D, rw);
-            Raw<float, N, AL> rb;
+            if (live) store_row<T, NT, W, C, AL>(static_cast<T*>(g.dx) + i * b.ld_x, l, D, dH);
+        }
+        // the group's sums on x's side
+        if (!g.gate && !g.post_w && !g.post_b) continue;
+        combine(t1);
+        if constexpr (LAYER) combine(t0);
+        float v[N];
+        if (g.gate) {
+            Raw<float, N, AL> rw, rb;
+            if (post) load_raw<float, NT, W, C, AL>(b.post_w, l, D, rw);
             if (LAYER && b.post_b) load_raw<float, NT, W, C, AL>(b.post_b, l, D, rb);
-            float s[M] = {};
 #pragma unroll
             for (int k = 0; k < N; ++k) {
-                const float xh = elem<NT, W, AL>(l, k) < D ? (raw_at(rx, k) - st.x) * st.y : 0.f;
-                const float p = du[k] * raw_at(rw, k);
-                s[0] = fmaf(p, xh, s[0]);
-                if (LAYER) s[M - 1] += p;
-                if (live) {
-                    float u = xh * raw_at(rw, k);
-                    if (LAYER && b.post_b) u += raw_at(rb, k);
-                    gt[k] = fmaf(b.scale * dH[k], u, gt[k]);
-                    qw[k] = fmaf(du[k], xh, qw[k]);
-                    if (LAYER) qb[k] += du[k];
+                v[k] = post ? raw_at(rw, k) * t1[k] : t1[k];
+                if constexpr (LAYER)
+                    if (b.post_b) v[k] = fmaf(raw_at(rb, k), t0[k], v[k]);
+                v[k] *= b.scale;
+            }
+            if (b.gate_rows && q.pieces == 1) {   // the whole group was here
+                if (rs == 0)
+                    store_row<float, NT, W, C, AL>(g.gate + (base / b.gate_rows) * D, l, D, v);
+            } else {
+                put(PL_GATE, v);
+            }
+        }
+        if (g.post_w || g.post_b) {
+            Raw<float, N, AL> rg;
+            if (gate) load_raw<float, NT, W, C, AL>(gate, l, D, rg);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const float f = gate ? b.scale * raw_at(rg, k) : b.scale;
+                t1[k] *= f;
+                if constexpr (LAYER) t0[k] *= f;
+                if constexpr (MANY) {
+                    qw[k] += t1[k];
+                    if constexpr (LAYER) qb[k] += t0[k];
                 }
             }
-            if (!g.dx) continue;   // (the same in every thread)
-            row_sum<NT, M>(s, red, slot);
-            const float c1 = s[0] * inv_d, c0 = LAYER ? s[M - 1] * inv_d : 0.f;
-#pragma unroll
-            for (int k = 0; k < N; ++k)
-                du[k] = st.y * (du[k] * raw_at(rw, k) - c0 - (raw_at(rx, k) - st.x) * st.y * c1);
-            if (live) store_row<T, NT, W, C, AL>(static_cast<T*>(g.dx) + i * b.ld_x, l, D, du);
         }
-        if (g.gate && b.gate_rows && q.pieces == 1) {   // the whole group was here
-            combine(gt);
-            if (rs == 0)
-                store_row<float, NT, W, C, AL>(g.gate + (base / b.gate_rows) * D, l, D, gt);
+        if constexpr (MANY) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) gt[k] = 0.f;
+            for (int k = 0; k < N; ++k) {
+                t1[k] = 0.f;
+                if constexpr (LAYER) t0[k] = 0.f;
+            }
         }
     }
-    float* out = part + (long long)blockIdx.x * kPlanes * q.Dp;
-    auto put = [&](bool wanted, int plane, float (&v)[N]) {
-        if (!wanted) return;
-        combine(v);
-        if (rs == 0) store_row<float, NT, W, C, AL>(out + (long long)plane * q.Dp, l, D, v);
-    };
-    put(g.pre_w, PL_PRE_W, pw);
-    put(g.post_w, PL_POST_W, qw);
-    put(g.gate && !(b.gate_rows && q.pieces == 1), PL_GATE, gt);
+    if (g.pre_w) {
+        combine(pw);
+        put(PL_PRE_W, pw);
+    }
+    if constexpr (MANY) {
+        if (g.post_w) put(PL_POST_W, qw);
+    } else {
+        if (g.post_w) put(PL_POST_W, t1);
+    }
     if constexpr (LAYER) {
-        put(g.pre_b, PL_PRE_B, pb);
-        put(g.post_b, PL_POST_B, qb);
+        if (g.pre_b) {
+            combine(pb);
+            put(PL_PRE_B, pb);
+        }
+        if constexpr (MANY) {
+            if (g.post_b) put(PL_POST_B, qb);
+        } else {
+            if (g.post_b) put(PL_POST_B, t0);
+        }
     }
 }
 
@@ -540,8 +626,12 @@ hipError_t block_norm_bwd(const BlockNorm& b, int R, const BlockNormGrads& g, vo
             constexpr int W = kRun<T, LAYER, AL>;
             with_row_shape<W>(b.D, [&](auto nt, auto c) {
                 constexpr int NT = decltype(nt)::value, C = decltype(c)::value;
-                hipLaunchKernelGGL((norm_bwd_kernel<T, W, NT, C, AL, LAYER>),
-                                   dim3((unsigned)q.blocks), dim3(block_of(NT)), 0, s, b, g, q, part);
+                if (q.gpb > 1)
+                    hipLaunchKernelGGL((norm_bwd_kernel<T, W, NT, C, AL, LAYER, true>),
+                                       dim3((unsigned)q.blocks), dim3(block_of(NT)), 0, s, b, g, q, part);
+                else
+                    hipLaunchKernelGGL((norm_bwd_kernel<T, W, NT, C, AL, LAYER, false>),
+                                       dim3((unsigned)q.blocks), dim3(block_of(NT)), 0, s, b, g, q, part);
             });
         };
         with_form(b, al, go);
