@@ -398,7 +398,8 @@ void mtx_free_model(mtx_model* m);
 /* Embedding lookup with scaling:  y[i][:] = scale * w[tokens[i]][:],  i < n, rounded once to
  * y_type; w [V][D] contiguous of w_type, y rows ldy >= D apart.  A token equal to `pad` gives a
  * row of zeros (pad < 0: no padding token); any other token outside [0, V) gives a row of NaN.
- * n = 0 does nothing.  V, D >= 1, V <= 2^28, n <= 2^30, n*D <= 2^36. */
+ * n = 0 does nothing.  V, D >= 1, V <= 2^28, D <= 2^24, n <= 2^30,
+ * n*D <= 2^36. */
 int mtx_embed_forward(const void* w, int w_type, int V, int D, const int32_t* tokens, size_t n,
                       int pad, float scale, void* y, int y_type, size_t ldy, void* stream);
 
@@ -429,7 +430,7 @@ int mtx_embed_backward(const int32_t* tokens, size_t n, int R, const void* dy, i
  *                  sequence's gate); must divide the rows of a shard.
  * Weights and gates are fp32.  ld_h, ld_x, ld_y: strides between rows (0: D) of h and h_out (and
  * dh, dh_out), of x (dx), of y (dy).  1 <= D <= 16384, rows < 2^31 (rows = 0 does nothing),
- * eps >= 0. */
+ * eps >= 0 (a row of zeros with eps = 0 gives NaN). */
 typedef enum { MTX_NORM_RMS = 0, MTX_NORM_LAYER = 1 } mtx_norm_kind;
 typedef struct {
     int kind;     /* mtx_norm_kind */
@@ -460,7 +461,7 @@ int mtx_block_norm_sizes(const mtx_norm_desc* d, int R, size_t* workspace_bytes)
  *   d_post_w, d_post_b, d_pre_w, d_pre_b (each nullable): parameter gradients of shard r, the
  *   sums over rows r*rows/R .. (r+1)*rows/R - 1, at [r*ld .. r*ld + D - 1] of each pointer;
  *   d_gate (nullable): likewise for gate_rows = 0, else [rows / gate_rows][D] without stride.
- * R must divide rows.  A gradient of an absent operand must be NULL. */
+ * R <= 65536 must divide rows.  A gradient of an absent operand must be NULL. */
 int mtx_block_norm_backward(const mtx_norm_desc* d, int R, const void* h_out, const void* x,
                             const float* stats, const void* dy, const void* dh_out, void* dh,
                             void* dx, float* d_post_w, float* d_post_b, float* d_gate,
@@ -483,7 +484,7 @@ int mtx_average_clip(const float* grads, int R, size_t n, size_t ld, float max_n
 /* The same over a list of tensors of either type.  Each is `n` contiguous elements at src (n may
  * be 0); dst receives the clipped elements, rounded to dst_type: dst = src (same type) clips in
  * place, dst = NULL only counts towards the norm.  No dst may overlap another tensor's src or
- * dst.  The handle keeps the list in the caller's workspace (mtx_clip_sizes bytes, 256-byte
+ * dst, nor norm_out any of them.  The handle keeps the list in the caller's workspace (mtx_clip_sizes bytes, 256-byte
  * aligned), which with the tensors must stay valid until mtx_free_clip; mtx_init_clip copies it
  * there and synchronises with `stream`.  A handle must not be used on two streams at once. */
 typedef struct {

@@ -6,7 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>
-#include <new>
+#include <utility>
 #include <vector>
 
 #include "api_common.h"
@@ -44,10 +44,12 @@ bool spans_overlap(std::initializer_list<Span> list)
 
 constexpr size_t kMaxRows = 2147483647;
 constexpr size_t kMaxTokens = (size_t)1 << 30;
+constexpr int kMaxEmbedD = 1 << 24;
 
 int check_embed(int V, int D, size_t n, int R)
 {
     if (V < 1 || D < 1) return fail(MTX_EINVAL, "V and D must be >= 1 (got %d, %d)", V, D);
+    if (D > kMaxEmbedD) return fail(MTX_EINVAL, "D must be at most %d (got %d)", kMaxEmbedD, D);
     if (R < 1 || R > 65536) return fail(MTX_EINVAL, "R must lie in 1 .. 65536 (got %d)", R);
     if (n > kMaxTokens || n * (size_t)R > kMaxTokens)
         return fail(MTX_EINVAL, "more than 2^30 tokens");
@@ -213,7 +215,8 @@ int mtx_block_norm_sizes(const mtx_norm_desc* d, int R, size_t* workspace_bytes)
     BlockNorm b{};
     const int rc = check_norm(d, b);
     if (rc) return rc;
-    if (R < 1 || b.rows % R) return fail(MTX_EINVAL, "R must be >= 1 and divide rows");
+    if (R < 1 || R > 65536 || b.rows % R)
+        return fail(MTX_EINVAL, "R must lie in 1 .. 65536 and divide rows");
     if (b.gate_rows && (b.rows / R) % b.gate_rows)
         return fail(MTX_EINVAL, "gate_rows must divide the rows of a shard");
     *workspace_bytes = block_norm_bwd_bytes(b, R);
@@ -229,7 +232,8 @@ int mtx_block_norm_backward(const mtx_norm_desc* d, int R, const void* h_out, co
     BlockNorm b{};
     const int rc = check_norm(d, b);
     if (rc) return rc;
-    if (R < 1 || b.rows % R) return fail(MTX_EINVAL, "R must be >= 1 and divide rows");
+    if (R < 1 || R > 65536 || b.rows % R)
+        return fail(MTX_EINVAL, "R must lie in 1 .. 65536 and divide rows");
     if (b.gate_rows && (b.rows / R) % b.gate_rows)
         return fail(MTX_EINVAL, "gate_rows must divide the rows of a shard");
     if (dy && !b.pre_w) return fail(MTX_EINVAL, "dy needs pre_w");
@@ -298,7 +302,7 @@ int mtx_block_norm_backward(const mtx_norm_desc* d, int R, const void* h_out, co
         for (const Span& a : in_out)
             if (pg[i] && a.bytes && overlap(pg[i], i == 2 ? gb : pb, a.p, a.bytes))
                 return fail(MTX_EINVAL, "a parameter gradient overlaps another tensor");
-    const BlockNormGrads g{h_out, x, stats, dy, dh_out, dh, dx, d_post_w, d_post_b, d_gate,
+    const BlockNormGrads g{h_out, want_x ? x : nullptr, stats, dy, dh_out, dh, dx, d_post_w, d_post_b, d_gate,
                            d_pre_w, d_pre_b, (long long)ld, false};
     HIP_TRY(block_norm_bwd(b, R, g, workspace, static_cast<hipStream_t>(stream)),
             "mtx_block_norm_backward");
@@ -335,6 +339,7 @@ int mtx_average_clip(const float* grads, int R, size_t n, size_t ld, float max_n
 
 struct mtx_clip {
     int chunks;
+    std::vector<std::pair<uintptr_t, uintptr_t>> spans;   // what the handle uses: disjoint, ascending
     bool in_place;   // every dst is its src or NULL: nothing to write where nothing is clipped
     double* part;
     ClipChunk* table;
@@ -445,7 +450,28 @@ int mtx_init_clip(const mtx_tensor* tensors, int count, void* workspace, size_t 
                 table.push_back(k);
             }
         }
+        std::vector<std::pair<uintptr_t, uintptr_t>> spans;
+        auto add_span = [&](const void* p, size_t bytes) {
+            const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+            if (p && bytes) spans.emplace_back(a, a + bytes);
+        };
+        add_span(workspace, need);
+        for (int i = 0; i < count; ++i) {
+            add_span(tensors[i].src, tensors[i].n * type_size(tensors[i].src_type));
+            if (tensors[i].dst)
+                add_span(tensors[i].dst, tensors[i].n * type_size(tensors[i].dst_type));
+        }
+        std::sort(spans.begin(), spans.end());
+        size_t kept = 0;
+        for (const auto& p : spans) {
+            if (kept && p.first <= spans[kept - 1].second)
+                spans[kept - 1].second = std::max(spans[kept - 1].second, p.second);
+            else
+                spans[kept++] = p;
+        }
+        spans.resize(kept);
         mtx_clip* c = new mtx_clip;
+        c->spans = std::move(spans);
         c->chunks = (int)table.size();
         c->in_place = in_place;
         c->part = static_cast<double*>(workspace);
@@ -473,6 +499,13 @@ int mtx_clip_grads(mtx_clip* c, float max_norm, float* norm_out, void* stream)
     if (!c) return fail(MTX_EINVAL, "the handle is NULL");
     if (!(max_norm > 0.0f)) return fail(MTX_EINVAL, "max_norm must be > 0");
     if (!aligned(norm_out, 4)) return fail(MTX_EINVAL, "norm_out must be 4-byte aligned");
+    if (norm_out) {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(norm_out);
+        // the last span that begins before norm_out ends
+        auto it = std::lower_bound(c->spans.begin(), c->spans.end(), std::make_pair(a + 4, (uintptr_t)0));
+        if (it != c->spans.begin() && (--it)->second > a)
+            return fail(MTX_EINVAL, "norm_out overlaps a tensor of the list or the workspace");
+    }
     c->last_stream = static_cast<hipStream_t>(stream);
     HIP_TRY(clip_list(c->table, c->chunks, c->in_place, max_norm, norm_out, c->part,
                       c->last_stream), "mtx_clip_grads");

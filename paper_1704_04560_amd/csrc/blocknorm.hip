@@ -153,21 +153,23 @@ constexpr int block_of(int NT) { return NT < 256 ? 256 : NT; }
 
 template <typename T, int W, int NT, int C, bool AL, bool LAYER>
 __global__ __launch_bounds__(block_of(NT)) void norm_fwd_kernel(BlockNorm b, const T* h, const T* x,
-                                                                T* h_out, T* y, float* stats)
+                                                                T* h_out, T* y, float* stats,
+                                                                long long row0)
 {
     constexpr int N = W * C, RPB = block_of(NT) / NT;
     __shared__ float red[2][1][16];
     int slot = 0;
     const int l = threadIdx.x % NT, D = b.D;
     const float inv_d = 1.0f / (float)D;
-    // (a block's rows run together: those past the end repeat the last one, storing nothing)
-    const long long want = (long long)blockIdx.x * RPB +
+    // (a block's rows run together: one past the end is as wide as nothing, read and written)
+    const long long want = row0 + (long long)blockIdx.x * RPB +
                            __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
     const bool live = want < b.rows;
     const long long i = live ? want : b.rows - 1;
+    const int Dl = live ? D : 0;
     Raw<T, N, AL> rh, rx;
-    load_raw<T, NT, W, C, AL>(h + i * b.ld_h, l, D, rh);
-    if (x) load_raw<T, NT, W, C, AL>(x + i * b.ld_x, l, D, rx);
+    load_raw<T, NT, W, C, AL>(h + i * b.ld_h, l, Dl, rh);
+    if (x) load_raw<T, NT, W, C, AL>(x + i * b.ld_x, l, Dl, rx);
     auto norm = [&](float (&v)[N], const float* w, const float* bias, int stat) {
         float s[1], mean = 0.f;
         if constexpr (LAYER) {
@@ -213,11 +215,11 @@ __global__ __launch_bounds__(block_of(NT)) void norm_fwd_kernel(BlockNorm b, con
 #pragma unroll
             for (int k = 0; k < N; ++k) H[k] = fmaf(b.scale, u[k], H[k]);
         }
-        if (h_out && live) store_row<T, NT, W, C, AL>(h_out + i * b.ld_h, l, D, H);
+        if (h_out) store_row<T, NT, W, C, AL>(h_out + i * b.ld_h, l, Dl, H);
     }
     if (!y) return;
     norm(H, b.pre_w, b.pre_b, 2);
-    if (live) store_row<T, NT, W, C, AL>(y + i * b.ld_y, l, D, H);
+    store_row<T, NT, W, C, AL>(y + i * b.ld_y, l, Dl, H);
 }
 
 static bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -271,10 +273,15 @@ hipError_t block_norm_fwd(const BlockNorm& b, const void* h, const void* x, void
         with_row_shape<W>(b.D, [&](auto nt, auto c) {
             constexpr int NT = decltype(nt)::value, C = decltype(c)::value;
             constexpr int RPB = block_of(NT) / NT;
-            hipLaunchKernelGGL((norm_fwd_kernel<T, W, NT, C, AL, LAYER>),
-                               dim3((unsigned)((b.rows + RPB - 1) / RPB)), dim3(block_of(NT)), 0, s,
-                               b, static_cast<const T*>(h), static_cast<const T*>(x),
-                               static_cast<T*>(h_out), static_cast<T*>(y), stats);
+            // (a launch has at most 2^32 threads)
+            constexpr long long most = 1LL << 21;
+            for (long long r = 0; r < b.rows; r += most * RPB) {
+                const long long n = std::min(most, (b.rows - r + RPB - 1) / RPB);
+                hipLaunchKernelGGL((norm_fwd_kernel<T, W, NT, C, AL, LAYER>), dim3((unsigned)n),
+                                   dim3(block_of(NT)), 0, s, b, static_cast<const T*>(h),
+                                   static_cast<const T*>(x), static_cast<T*>(h_out),
+                                   static_cast<T*>(y), stats, r);
+            }
         });
     };
     with_form(b, al, go);
@@ -385,28 +392,32 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
     auto put = [&](int plane, const float (&v)[N]) {
         if (rs == 0) store_row<float, NT, W, C, AL>(out + (long long)plane * q.Dp, l, D, v);
     };
+    // (a slot past the rows: as wide as nothing, read and written)
     auto row_of = [&](long long gi, int j0) {
         return shard * nb + gi * q.group + first + (j0 + rs < rows ? j0 + rs : 0);
     };
+    auto width = [&](int j0) { return j0 + rs < rows ? D : 0; };
     Raw<T, N, AL> rH, ry;
-    auto load_y = [&](long long i) {
-        load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.dy) + i * b.ld_y, l, D, ry);
-        load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.h_out) + i * b.ld_h, l, D, rH);
+    auto load_y = [&](long long gi, int j0) {
+        const long long i = row_of(gi, j0);
+        load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.dy) + i * b.ld_y, l, width(j0), ry);
+        load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.h_out) + i * b.ld_h, l, width(j0), rH);
     };
-    if (has_y && rows && g0 < g1) load_y(row_of(g0, 0));
+    if (has_y && rows && g0 < g1) load_y(g0, 0);
     for (long long gi = g0; gi < g1; gi += gstep) {
         const long long base = shard * nb + gi * q.group;
         const float* gate = b.gate ? b.gate + (b.gate_rows ? base / b.gate_rows : 0) * D : nullptr;
         for (int j0 = 0; j0 < rows; j0 += RPB) {
             const bool live = j0 + rs < rows;
             const long long i = row_of(gi, j0);
+            const int Dl = width(j0);
             Raw<T, N, AL> ro, rx;
             Raw<float, N, AL> rw;
             float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
             if (g.stats) st = *reinterpret_cast<const float4*>(g.stats + 4 * i);
             if (g.dh_out)
-                load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.dh_out) + i * b.ld_h, l, D, ro);
-            if (has_x) load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.x) + i * b.ld_x, l, D, rx);
+                load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.dh_out) + i * b.ld_h, l, Dl, ro);
+            if (has_x) load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.x) + i * b.ld_x, l, Dl, rx);
             // the row's loads are issued here, not moved behind the sums
             __builtin_amdgcn_sched_barrier(0);
             float dH[N];
@@ -435,19 +446,19 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
 #pragma unroll
                 for (int k = 0; k < N; ++k) dH[k] = raw_at(ro, k);
             }
-            if (g.dh && live) {
+            if (g.dh) {
                 if (g.relu_h) {
                     float v[N];
 #pragma unroll
                     for (int k = 0; k < N; ++k) v[k] = raw_at(rH, k) > 0.f ? dH[k] : 0.f;
-                    store_row<T, NT, W, C, AL>(static_cast<T*>(g.dh) + i * b.ld_h, l, D, v);
+                    store_row<T, NT, W, C, AL>(static_cast<T*>(g.dh) + i * b.ld_h, l, Dl, v);
                 } else {
-                    store_row<T, NT, W, C, AL>(static_cast<T*>(g.dh) + i * b.ld_h, l, D, dH);
+                    store_row<T, NT, W, C, AL>(static_cast<T*>(g.dh) + i * b.ld_h, l, Dl, dH);
                 }
             }
             if (has_y) {
-                if (j0 + RPB < rows) load_y(row_of(gi, j0 + RPB));
-                else if (MANY && gi + 1 < g1) load_y(row_of(gi + 1, 0));
+                if (j0 + RPB < rows) load_y(gi, j0 + RPB);
+                else if (MANY && gi + 1 < g1) load_y(gi + 1, 0);
             }
             if (!has_x) continue;
             if (live) {
@@ -485,7 +496,7 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
                 for (int k = 0; k < N; ++k)
                     dH[k] = st.y * (dH[k] - c0 - (raw_at(rx, k) - st.x) * st.y * c1);
             }
-            if (live) store_row<T, NT, W, C, AL>(static_cast<T*>(g.dx) + i * b.ld_x, l, D, dH);
+            store_row<T, NT, W, C, AL>(static_cast<T*>(g.dx) + i * b.ld_x, l, Dl, dH);
         }
         // the group's sums on x's side
         if (!g.gate && !g.post_w && !g.post_b) continue;

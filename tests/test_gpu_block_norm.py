@@ -280,3 +280,41 @@ def test_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, out + [st, gr]))
+
+
+def test_many_rows_and_rows_past_32_bits():
+    """More rows than one launch takes threads (2^26 + 5 rows of one element), and rows 2^28 apart."""
+    N = (1 << 26) + 5
+    print(f"[case] block_norm N={N} D=1", flush=True)
+    p = _dev(_params(_gen(1), 1, False, False, False, 1))
+    d = _desc(mtx.MTX_NORM_RMS, BF16, N, 1, 1.0, 0, p)
+    h = torch.arange(N, device="cuda", dtype=torch.float32).remainder_(1000).add_(1).to(BF16).view(N, 1)
+    y = torch.zeros_like(h)
+    mtx.mtx_block_norm_forward(d, h, None, None, y, None)
+    f = h[:1000].double()
+    want = f / (f * f + EPS).sqrt() * p["pre_w"].double()
+    got = y[:N - N % 1000].view(-1, 1000).float()
+    assert (got.amax(0) == got.amin(0)).all()   # every repetition gives the same bits
+    assert_within(got[0], want[:, 0], want[:, 0].abs() * (half(BF16) + 8 * U), "y")
+    assert torch.equal(y[-(N % 1000):], y[:N % 1000])
+    del h, y
+    ld, N, D = 1 << 28, 10, 520
+    g = _gen(2)
+    p = _dev(_params(g, D, True, True, True, 1))
+    t = torch.zeros(2, N, ld, dtype=BF16, device="cuda")
+    t[:, :, :D] = torch.randn(2, N, D, generator=g).to(BF16).cuda()
+    small = t[:, :, :D].contiguous()
+    outs = []
+    for k, (a, l) in enumerate(((t, ld), (small, D))):
+        d = _desc(mtx.MTX_NORM_LAYER, BF16, N, D, 1.0, 0, p, (l, l, l))
+        st = torch.empty(N, 4, device="cuda")
+        y = torch.zeros_like(a[0])
+        mtx.mtx_block_norm_forward(d, a[0], a[1], a[0], y, st)
+        gr, ws = torch.empty(5, D, device="cuda"), torch.empty(mtx.mtx_block_norm_sizes(d, 1),
+                                                               dtype=torch.uint8, device="cuda")
+        dx = torch.zeros_like(a[0])
+        mtx.mtx_block_norm_backward(d, 1, a[0], a[1], st, y, None, None, dx, gr[0], gr[1], gr[2],
+                                    gr[3], gr[4], D, ws)
+        outs.append((a[0][:, :D].clone(), y[:, :D].clone(), dx[:, :D].clone(), st, gr))
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)

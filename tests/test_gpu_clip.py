@@ -172,3 +172,15 @@ def test_captured_and_replayed():
         graphs[0].replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(want, (out, avg, nrm)))
+
+
+def test_norm_out_inside_the_list_is_refused():
+    a = torch.ones(300, device="cuda")
+    b = torch.ones(300, device="cuda")
+    clip = mtx.Clip([(a[:100], None), (a[50:200], None), (b, b)])
+    for bad in (a[0:], a[199:], b[299:], b[150:], clip.workspace[64:]):
+        with pytest.raises(mtx.MtxError) as e:
+            clip.clip(1.0, bad)
+        assert e.value.code == mtx.MTX_EINVAL
+    clip.clip(1.0, a[200:])
+    assert abs(a[200].item() - 550 ** 0.5) <= 2 * U * 550 ** 0.5

@@ -67,6 +67,7 @@ CASES = [  # V, D, n, R, pad, scale, token law, extra lddy, offset, extra ld
     (3, 1, 9000, 1, 2, 1.0, "uniform", 0, 0, 0), (600, 256, 128, 8, -1, 1.0, "two", 0, 0, 0),
     (500, 200, 3001, 2, 0, 1.0, "zipf", 0, 0, 4), (300, 1032, 2500, 1, -1, 0.5, "zipf", 8, 0, 0),
     (900, 264, 1025, 3, -1, 1.0, "uniform", 0, 0, 0), (50, 16, 70000, 1, -1, 1.0, "one", 0, 0, 0),
+    (131072, 16, 300, 1, -1, 1.0, "zipf", 0, 0, 0), (1 << 20, 8, 2100, 1, 5, 1.0, "zipf", 0, 0, 0),
     (30, 128, 6000, 2, 29, 1.0, "two", 0, 0, 0), (40, 2056, 1024, 1, -1, 1.0, "one", 0, 0, 0),
 ]
 
@@ -162,3 +163,42 @@ def test_gradients_on_two_streams_and_replayed():
             s[2].fill_(7.0)
         graph.replay()
         check()
+
+
+@pytest.mark.parametrize("acc", [False, True])
+@pytest.mark.parametrize("n", [50, 3000])
+def test_only_padding(n, acc):
+    V, D = 300, 40
+    tok = torch.full((2 * n,), 7, dtype=torch.int32, device="cuda")
+    dy = torch.full((2 * n, D), float("nan"), device="cuda")
+    start = torch.randn(2, V * D, generator=_gen(1)).cuda()
+    grads = start.clone()
+    _bwd(tok, n, 2, dy, D, V, D, 7, 1.0, grads, V * D, acc)
+    assert torch.equal(grads, start if acc else torch.zeros_like(start))
+
+
+def test_tables_and_rows_past_32_bits():
+    """2.4e9 table elements, and rows of y and dy 2^26 elements apart."""
+    V, D, n = 300_000, 8192, 40
+    tok = torch.tensor([0, V - 1, V // 2, 299_000, 7] * 8, dtype=torch.int32, device="cuda")
+    print("[case] embed V*D = 2.4e9", flush=True)
+    w = torch.zeros(V, D, dtype=BF16, device="cuda")
+    w[tok.long()] = torch.randn(n, D, generator=_gen(2)).to(BF16).cuda()
+    ld = 1 << 26
+    y = torch.zeros(n, ld, dtype=BF16, device="cuda")
+    mtx.mtx_embed_forward(w, MT[BF16], V, D, tok, n, -1, 1.0, y, MT[BF16], ld)
+    assert torch.equal(y[:, :D], w[tok.long()])
+    del w
+    grads = torch.ones(V, D, device="cuda")
+    _bwd(tok, n, 1, y, ld, V, D, -1, 1.0, grads, V * D, False)
+    ref, mag, cnt = embed_grad((tok.cpu().long() % 1009), y[:, :D].cpu(), 1009, -1, 1.0)
+    rows = torch.unique(tok.cpu().long())   # (distinct modulo 1009)
+    assert_within(grads[rows.cuda()], ref[rows % 1009], U * (cnt + 3)[rows % 1009] * mag[rows % 1009], "rows")
+    grads[rows.cuda()] = 0.0
+    assert not grads.any()
+    big = tok.repeat(30)
+    del y
+    dy = torch.randn(1200, D, generator=_gen(3)).cuda()
+    _bwd(big, 1200, 1, dy, D, V, D, -1, 1.0, grads, V * D, True)
+    ref, mag, cnt = embed_grad((big.cpu().long() % 1009), dy.cpu(), 1009, -1, 1.0)
+    assert_within(grads[rows.cuda()], ref[rows % 1009], U * (cnt + 3)[rows % 1009] * mag[rows % 1009], "rows")

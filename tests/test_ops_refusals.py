@@ -31,7 +31,8 @@ def test_embed_forward():
     for bad in (dict(w=None), dict(tok=None), dict(y=None), dict(V=0), dict(D=0), dict(wt=2),
                 dict(yt=-1), dict(ldy=7), dict(scale=math.nan), dict(n=1 << 31),
                 dict(w=A[0] + 2), dict(tok=A[1] + 2), dict(y=A[2] + 1), dict(y=A[0] + 16),
-                dict(y=A[1] - 8), dict(ldy=1 << 62)):
+                dict(y=A[1] - 8), dict(ldy=1 << 62),
+                dict(D=(1 << 24) + 1, ldy=1 << 25)):
         assert call(**bad) == mtx.MTX_EINVAL, bad
 
 
@@ -109,7 +110,7 @@ def test_block_norm_backward():
     small = Buf(A[7])
     small.nbytes = size - 1
     assert call(ws=small) == mtx.MTX_ENOMEM
-    for R in (0, 5):
+    for R in (0, 5, 65537):
         with pytest.raises(mtx.MtxError):
             mtx.mtx_block_norm_sizes(desc(), R)
 
