@@ -46,38 +46,13 @@ __device__ __forceinline__ float clip_factor(const double* part, int np, const C
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-template <bool EXACT>
-__global__ __launch_bounds__(256) void avg_sq_scalar(const float* __restrict__ grads, int R,
-                                                     long long n, long long ld,
-                                                     float* __restrict__ avg,
-                                                     double* __restrict__ part)
-{
-    __shared__ double red[4];
-    double acc = 0.0;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n;
-         i += (long long)gridDim.x * 256) {
-        float g;
-        if (EXACT) {
-            double s = (double)grads[i];
-            for (int r = 1; r < R; ++r) s += (double)grads[(long long)r * ld + i];
-            g = (float)(s / (double)R);
-        } else {
-            float s = grads[i];
-            for (int r = 1; r < R; ++r) s += grads[(long long)r * ld + i];
-            g = s / (float)R;
-        }
-        avg[i] = g;
-        acc = fma((double)g, (double)g, acc);
-    }
-    acc = block_sum(acc, red);
-    if (threadIdx.x == 0) part[blockIdx.x] = acc;
-}
-
 // 16-byte vectors, two per thread and pass, 4 KB apart; the rows are read once (nontemporal).  The
 // average is read again by the second launch; it is written through the caches, or past them where
-// the rows' traffic would push it out (PAST).  The n % 4 elements left over: the grid's first thread.
-// 16 x 61M: 697 us, 5.95 TB/s.
-template <int RT, bool EXACT, bool PAST>
+// the rows' traffic would push it out (AVG_PAST).  The n % 4 elements left over: the grid's first
+// thread.  AVG_UNALIGNED: rows or an average that start at any element (unaligned
+// vectors: 16 x 5M 72 us, single ones 99).  16 x 61M: 697 us, 5.95 TB/s.
+enum Avg { AVG_CACHED, AVG_PAST, AVG_UNALIGNED };
+template <int RT, bool EXACT, Avg HOW>
 __global__ __launch_bounds__(256) void avg_sq_vec4(const float* __restrict__ grads, int Rrt,
                                                    long long n, long long ld,
                                                    float* __restrict__ avg,
@@ -87,8 +62,8 @@ __global__ __launch_bounds__(256) void avg_sq_vec4(const float* __restrict__ gra
     constexpr int U = 2;
     __shared__ double red[4];
     const int R = RT > 0 ? RT : Rrt;
-    const long long n4 = n / 4, ld4 = ld / 4;
-    const f32x4* g4 = reinterpret_cast<const f32x4*>(grads);
+    typedef float uf32x4 __attribute__((ext_vector_type(4), aligned(4)));
+    const long long n4 = n / 4;
     double acc = 0.0;
     for (long long base = (long long)blockIdx.x * 256 * U; base < n4;
          base += (long long)gridDim.x * 256 * U) {
@@ -104,7 +79,10 @@ __global__ __launch_bounds__(256) void avg_sq_vec4(const float* __restrict__ gra
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (ok[u]) {
-                    const f32x4 x = __builtin_nontemporal_load(g4 + r * ld4 + base + u * 256 + threadIdx.x);
+                    const float* p = grads + r * ld + 4 * (base + u * 256 + threadIdx.x);
+                    const f32x4 x = HOW == AVG_UNALIGNED
+                                        ? __builtin_nontemporal_load(reinterpret_cast<const uf32x4*>(p))
+                                        : __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
 #pragma unroll
                     for (int j = 0; j < 4; ++j) s[u][j] = r == 0 ? (A)x[j] : s[u][j] + (A)x[j];
                 }
@@ -124,9 +102,10 @@ __global__ __launch_bounds__(256) void avg_sq_vec4(const float* __restrict__ gra
                 g[j] = (float)(s[u][j] / (A)R);
                 acc = fma((double)g[j], (double)g[j], acc);
             }
-            f32x4* out = reinterpret_cast<f32x4*>(avg) + base + u * 256 + threadIdx.x;
-            if (PAST) __builtin_nontemporal_store(g, out);
-            else *out = g;
+            float* out = avg + 4 * (base + u * 256 + threadIdx.x);
+            if (HOW == AVG_PAST) __builtin_nontemporal_store(g, reinterpret_cast<f32x4*>(out));
+            else if (HOW == AVG_CACHED) *reinterpret_cast<f32x4*>(out) = g;
+            else *reinterpret_cast<uf32x4*>(out) = g;
         }
     }
     if (blockIdx.x == 0 && threadIdx.x == 0)
@@ -142,43 +121,39 @@ __global__ __launch_bounds__(256) void avg_sq_vec4(const float* __restrict__ gra
 }
 
 // From the end of the vector to its start: what the first launch wrote last is still in the cache.
-template <bool VEC>
-__global__ __launch_bounds__(256) void scale_kernel(float* __restrict__ g, long long n,
+// `head` elements lie before the first aligned vector.
+__global__ __launch_bounds__(256) void scale_kernel(float* __restrict__ g, long long n, int head,
                                                     const double* __restrict__ part, int np,
                                                     ClipOut o)
 {
     const float f = clip_factor(part, np, o);
     if (f == 1.0f) return;
-    const long long step = (long long)gridDim.x * 256, n4 = VEC ? n / 4 : 0;
+    const long long step = (long long)gridDim.x * 256, n4 = (n - head) / 4;
     const long long t = (long long)blockIdx.x * 256 + threadIdx.x;
-    f32x4* g4 = reinterpret_cast<f32x4*>(g);
+    f32x4* g4 = reinterpret_cast<f32x4*>(g + head);
 #pragma unroll 2
     for (long long i = n4 - 1 - t; i >= 0; i -= step) g4[i] *= f;
-    for (long long i = 4 * n4 + t; i < n; i += step) g[i] *= f;
+    if (t < head) g[t] *= f;
+    if (head + 4 * n4 + t < n) g[head + 4 * n4 + t] *= f;
 }
 
 template <bool EXACT>
 static void launch_avg_sq(const float* grads, int R, long long n, long long ld, float* avg,
-                          double* part, unsigned blocks, bool vec, hipStream_t s)
+                          double* part, unsigned blocks, bool al, hipStream_t s)
 {
     // (LDS that keeps five blocks to a compute unit, as in the averages without a norm)
     const size_t lds = 160 * 1024 / 5 - 1024;
     // Average, clip and update: 4 x 30M (600 MB) 230 us through the caches, 236 past them; 16 x 16M
     // (1.1 GB) 264 and 248.
-    const bool past = (double)n * (R + 1) * 4 > 768e6;
+    const Avg how = !al ? AVG_UNALIGNED : (double)n * (R + 1) * 4 > 768e6 ? AVG_PAST : AVG_CACHED;
     auto go = [&](auto rt) {
         constexpr int RT = decltype(rt)::value;
-        if (past)
-            hipLaunchKernelGGL((avg_sq_vec4<RT, EXACT, true>), dim3(blocks), dim3(256), lds, s,
-                               grads, R, n, ld, avg, part);
-        else
-            hipLaunchKernelGGL((avg_sq_vec4<RT, EXACT, false>), dim3(blocks), dim3(256), lds, s,
-                               grads, R, n, ld, avg, part);
+        auto kernel = how == AVG_PAST     ? avg_sq_vec4<RT, EXACT, AVG_PAST>
+                      : how == AVG_CACHED ? avg_sq_vec4<RT, EXACT, AVG_CACHED>
+                                          : avg_sq_vec4<RT, EXACT, AVG_UNALIGNED>;
+        hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), lds, s, grads, R, n, ld, avg, part);
     };
-    if (!vec)
-        hipLaunchKernelGGL((avg_sq_scalar<EXACT>), dim3(blocks), dim3(256), 0, s, grads, R, n, ld,
-                           avg, part);
-    else if (R == 1) go(std::integral_constant<int, 1>());
+    if (R == 1) go(std::integral_constant<int, 1>());
     else if (R == 2) go(std::integral_constant<int, 2>());
     else if (R == 4) go(std::integral_constant<int, 4>());
     else if (R == 8) go(std::integral_constant<int, 8>());
@@ -189,24 +164,20 @@ static void launch_avg_sq(const float* grads, int R, long long n, long long ld, 
 hipError_t average_clip(const float* grads, int R, size_t n, size_t ld, bool exact, float max_norm,
                         float* avg, float* norm_out, int* nonfinite, double* part, hipStream_t s)
 {
-    auto al = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
-    const bool vec_avg = al(avg), vec = vec_avg && al(grads) && ld % 4 == 0;
-    const size_t per = vec ? 2048 : 256;
-    // five blocks to each of 256 compute units: more would run as a second, partly filled round
-    const unsigned blocks = (unsigned)std::min<size_t>(vec ? 1280 : kClipBlocks, (n + per - 1) / per);
-    if (exact) launch_avg_sq<true>(grads, R, n, ld, avg, part, blocks, vec, s);
-    else launch_avg_sq<false>(grads, R, n, ld, avg, part, blocks, vec, s);
+    const unsigned off = (unsigned)(reinterpret_cast<uintptr_t>(avg) & 15);
+    const bool al = !off && (reinterpret_cast<uintptr_t>(grads) & 15) == 0 && (ld % 4 == 0 || R == 1);
+    // at most five blocks to each of 256 compute units: more would run as a second, partly filled round
+    const unsigned blocks = (unsigned)std::min<size_t>(1280, (n + 2047) / 2048);
+    if (exact) launch_avg_sq<true>(grads, R, n, ld, avg, part, blocks, al, s);
+    else launch_avg_sq<false>(grads, R, n, ld, avg, part, blocks, al, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     timing_split(s, "scale");
     const ClipOut o{max_norm, norm_out, nonfinite};
     const unsigned sblocks = (unsigned)std::min<size_t>(kClipBlocks, (n + 1023) / 1024);
-    if (vec_avg)
-        hipLaunchKernelGGL((scale_kernel<true>), dim3(sblocks), dim3(256), 0, s, avg, (long long)n,
-                           part, (int)blocks, o);
-    else
-        hipLaunchKernelGGL((scale_kernel<false>), dim3(sblocks), dim3(256), 0, s, avg, (long long)n,
-                           part, (int)blocks, o);
+    const int head = (int)std::min<size_t>(n, off ? (16 - off) / 4 : 0);
+    hipLaunchKernelGGL(scale_kernel, dim3(sblocks), dim3(256), 0, s, avg, (long long)n, head, part,
+                       (int)blocks, o);
     return hipGetLastError();
 }
 
