@@ -8,8 +8,8 @@
 // Statistics and sums are fp32; only h_out, y, dh and dx are rounded to the tensors' type.
 //
 // A row is held in the registers of NT threads, C times 16 bytes each, so that every tensor is read
-// and written once: both passes are bound by HBM.  Rows of at most 1 KB take one wave and need no
-// barrier.
+// and written once: both passes are bound by HBM.  Rows of at most 64 runs of elements take a wave,
+// of at most 16 or 32 a quarter or half of one, and need no barrier.
 #include "device_common.h"
 #include "internal.h"
 
@@ -38,21 +38,31 @@ template <typename T, int N, bool AL> struct Raw {
 
 // A row as a buffer of D elements: what lies past its end reads as zero and is not written, without a
 // branch or a mask for it (8850 rows of 771 fp32, backward: 53 -> 47 us).  The pointer is the same
-// in every lane of a wave.
-template <typename T> __device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const T* p, int D)
+// in every lane of a wave.  Where a wave holds several rows (NT < 64), each lane adds its row's
+// distance `off` (elements) from the wave's first, and names a place past any buffer for what its
+// row does not have.
+template <typename T, int NT>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const T* p, int D)
 {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p), 0, D * (int)sizeof(T), 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p), 0,
+                                             NT < 64 ? 0x7fffffff : D * (int)sizeof(T), 0x00020000);
+}
+
+template <typename T, int NT> __device__ __forceinline__ int row_byte(int d, int off, int D)
+{
+    if (NT >= 64) return d * (int)sizeof(T);
+    return d < D ? (off + d) * (int)sizeof(T) : (int)0x80000000;
 }
 
 template <typename T, int NT, int W, int C, bool AL>
-__device__ __forceinline__ void load_raw(const T* p, int l, int D, Raw<T, W * C, AL>& o)
+__device__ __forceinline__ void load_raw(const T* p, int l, int D, Raw<T, W * C, AL>& o, int off = 0)
 {
-    const __amdgpu_buffer_rsrc_t r = row_buffer(p, D);
+    const __amdgpu_buffer_rsrc_t r = row_buffer<T, NT>(p, D);
     if constexpr (AL) {
         constexpr int bytes = W * (int)sizeof(T);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int at = (c * NT + l) * bytes;
+            const int at = row_byte<T, NT>((c * NT + l) * W, off, D);
             if constexpr (bytes == 8) {
                 const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0);
                 o.w[2 * c] = v[0];
@@ -69,7 +79,7 @@ __device__ __forceinline__ void load_raw(const T* p, int l, int D, Raw<T, W * C,
     } else {
 #pragma unroll
         for (int k = 0; k < W * C; ++k) {
-            const int at = (k * NT + l) * (int)sizeof(T);
+            const int at = row_byte<T, NT>(k * NT + l, off, D);
             if constexpr (sizeof(T) == 4)
                 o.e[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0));
             else
@@ -87,14 +97,14 @@ __device__ __forceinline__ float raw_at(const Raw<T, N, AL>& o, int k)
 }
 
 template <typename T, int NT, int W, int C, bool AL>
-__device__ __forceinline__ void store_row(T* p, int l, int D, const float (&v)[W * C])
+__device__ __forceinline__ void store_row(T* p, int l, int D, const float (&v)[W * C], int off = 0)
 {
-    const __amdgpu_buffer_rsrc_t r = row_buffer(p, D);
+    const __amdgpu_buffer_rsrc_t r = row_buffer<T, NT>(p, D);
     if constexpr (AL) {
         constexpr int bytes = W * (int)sizeof(T);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int at = (c * NT + l) * bytes;
+            const int at = row_byte<T, NT>((c * NT + l) * W, off, D);
             T e[W];
 #pragma unroll
             for (int k = 0; k < W; ++k) e[k] = from_f32<T>(v[W * c + k]);
@@ -114,7 +124,7 @@ __device__ __forceinline__ void store_row(T* p, int l, int D, const float (&v)[W
     } else {
 #pragma unroll
         for (int k = 0; k < W * C; ++k) {
-            const int at = (k * NT + l) * (int)sizeof(T);
+            const int at = row_byte<T, NT>(k * NT + l, off, D);
             const T e = from_f32<T>(v[k]);
             if constexpr (sizeof(T) == 4)
                 __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, e), r, at, 0, 0);
@@ -132,7 +142,7 @@ __device__ __forceinline__ void row_sum(float (&v)[M], float (&red)[2][M][16], i
 #pragma unroll
     for (int m = 0; m < M; ++m)
 #pragma unroll
-        for (int o = 32; o; o >>= 1) v[m] += __shfl_xor(v[m], o);
+        for (int o = (NT < 64 ? NT : 64) / 2; o; o >>= 1) v[m] += __shfl_xor(v[m], o);
     if constexpr (NT > 64) {
         const int wave = threadIdx.x >> 6, first = threadIdx.x / NT * (NT / 64);
         if ((threadIdx.x & 63) == 0)
@@ -151,6 +161,18 @@ __device__ __forceinline__ void row_sum(float (&v)[M], float (&red)[2][M][16], i
 
 constexpr int block_of(int NT) { return NT < 256 ? 256 : NT; }
 
+// A block holds block_of(NT) / NT rows at a time, one to a slot.  first: the wave's first slot (the same
+// in all its lanes); sub: the lane's slot after it.
+struct Slot {
+    int first, sub;
+};
+template <int NT> __device__ __forceinline__ Slot row_slot()
+{
+    if (NT >= 64) return Slot{__builtin_amdgcn_readfirstlane(threadIdx.x / NT), 0};
+    return Slot{__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (64 / NT),
+                (int)(threadIdx.x & 63) / NT};
+}
+
 template <typename T, int W, int NT, int C, bool AL, bool LAYER>
 __global__ __launch_bounds__(block_of(NT)) void norm_fwd_kernel(BlockNorm b, const T* h, const T* x,
                                                                 T* h_out, T* y, float* stats,
@@ -162,14 +184,14 @@ __global__ __launch_bounds__(block_of(NT)) void norm_fwd_kernel(BlockNorm b, con
     const int l = threadIdx.x % NT, D = b.D;
     const float inv_d = 1.0f / (float)D;
     // (a block's rows run together: one past the end is as wide as nothing, read and written)
-    const long long want = row0 + (long long)blockIdx.x * RPB +
-                           __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
-    const bool live = want < b.rows;
-    const long long i = live ? want : b.rows - 1;
+    const Slot sl = row_slot<NT>();
+    const long long iw = row0 + (long long)blockIdx.x * RPB + sl.first, i = iw + sl.sub;
+    const bool live = i < b.rows;
     const int Dl = live ? D : 0;
+    const int oh = sl.sub * (int)b.ld_h, ox = sl.sub * (int)b.ld_x, oy = sl.sub * (int)b.ld_y;
     Raw<T, N, AL> rh, rx;
-    load_raw<T, NT, W, C, AL>(h + i * b.ld_h, l, Dl, rh);
-    if (x) load_raw<T, NT, W, C, AL>(x + i * b.ld_x, l, Dl, rx);
+    load_raw<T, NT, W, C, AL>(h + iw * b.ld_h, l, Dl, rh, oh);
+    if (x) load_raw<T, NT, W, C, AL>(x + iw * b.ld_x, l, Dl, rx, ox);
     auto norm = [&](float (&v)[N], const float* w, const float* bias, int stat) {
         float s[1], mean = 0.f;
         if constexpr (LAYER) {
@@ -208,18 +230,20 @@ __global__ __launch_bounds__(block_of(NT)) void norm_fwd_kernel(BlockNorm b, con
         if (b.post_w) norm(u, b.post_w, b.post_b, 0);
         if (b.gate) {
             Raw<float, N, AL> rg;
-            load_raw<float, NT, W, C, AL>(b.gate + (b.gate_rows ? i / b.gate_rows : 0) * D, l, D, rg);
+            const long long gw = b.gate_rows ? iw / b.gate_rows : 0;
+            const int og = NT < 64 && b.gate_rows ? (int)(i / b.gate_rows - gw) * D : 0;
+            load_raw<float, NT, W, C, AL>(b.gate + gw * D, l, Dl, rg, og);
 #pragma unroll
             for (int k = 0; k < N; ++k) H[k] = fmaf(b.scale * raw_at(rg, k), u[k], H[k]);
         } else {
 #pragma unroll
             for (int k = 0; k < N; ++k) H[k] = fmaf(b.scale, u[k], H[k]);
         }
-        if (h_out) store_row<T, NT, W, C, AL>(h_out + i * b.ld_h, l, Dl, H);
+        if (h_out) store_row<T, NT, W, C, AL>(h_out + iw * b.ld_h, l, Dl, H, oh);
     }
     if (!y) return;
     norm(H, b.pre_w, b.pre_b, 2);
-    store_row<T, NT, W, C, AL>(y + i * b.ld_y, l, Dl, H);
+    store_row<T, NT, W, C, AL>(y + iw * b.ld_y, l, Dl, H, oy);
 }
 
 static bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -249,16 +273,35 @@ static bool norm_vec(const BlockNorm& b, std::initializer_list<const void*> ptrs
     return ok;
 }
 
-// Calls f(NT, C) as constants: the threads of a row of W elements a thread and step.
-template <int W, class F> static void with_row_shape(int D, F f)
+// Threads of a row of D elements in runs of w (C = 1 up to 1024).  Rows that share a wave must lie within
+// the reach of its 31-bit distances: `far` is the largest one, in bytes.
+static int row_threads(int D, int w, double far)
 {
-        if (D <= 64 * W) f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
-    else if (D <= 128 * W) f(std::integral_constant<int, 128>(), std::integral_constant<int, 1>());
-    else if (D <= 256 * W) f(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
-    else if (D <= 512 * W) f(std::integral_constant<int, 512>(), std::integral_constant<int, 1>());
-    else if (D <= 1024 * W) f(std::integral_constant<int, 1024>(), std::integral_constant<int, 1>());
+    int nt = far < 2147483647.0 ? 16 : 64;
+    while (nt < 1024 && nt * w < D) nt *= 2;
+    return nt;
+}
+
+// Calls f(NT, C) as constants.
+template <int W, class F> static void with_row_shape(int D, int nt, F f)
+{
+    const std::integral_constant<int, 1> one;
+    if (nt == 16) f(std::integral_constant<int, 16>(), one);
+    else if (nt == 32) f(std::integral_constant<int, 32>(), one);
+    else if (nt == 64) f(std::integral_constant<int, 64>(), one);
+    else if (nt == 128) f(std::integral_constant<int, 128>(), one);
+    else if (nt == 256) f(std::integral_constant<int, 256>(), one);
+    else if (nt == 512) f(std::integral_constant<int, 512>(), one);
+    else if (D <= 1024 * W) f(std::integral_constant<int, 1024>(), one);
     else if (D <= 2048 * W) f(std::integral_constant<int, 1024>(), std::integral_constant<int, 2>());
     else f(std::integral_constant<int, 1024>(), std::integral_constant<int, W == 8 ? 2 : 4>());
+}
+
+// Largest distance in bytes of a tensor's rows that share a wave and lie `step` rows apart.
+static double wave_reach(const BlockNorm& b, long long step)
+{
+    const double ld = (double)std::max({b.ld_h, b.ld_x, b.ld_y});
+    return (3.0 * step + 1.0) * ld * (b.dt == DT_F32 ? 4 : 2);
 }
 
 hipError_t block_norm_fwd(const BlockNorm& b, const void* h, const void* x, void* h_out, void* y,
@@ -270,7 +313,7 @@ hipError_t block_norm_fwd(const BlockNorm& b, const void* h, const void* x, void
         using T = decltype(t);
         constexpr bool LAYER = decltype(layer)::value, AL = decltype(aligned)::value;
         constexpr int W = kRun<T, LAYER, AL>;
-        with_row_shape<W>(b.D, [&](auto nt, auto c) {
+        with_row_shape<W>(b.D, row_threads(b.D, W, wave_reach(b, 1)), [&](auto nt, auto c) {
             constexpr int NT = decltype(nt)::value, C = decltype(c)::value;
             constexpr int RPB = block_of(NT) / NT;
             // (a launch has at most 2^32 threads)
@@ -299,6 +342,7 @@ hipError_t block_norm_fwd(const BlockNorm& b, const void* h, const void* x, void
 struct NormDeal {
     long long group, groups_shard;   // rows of a group, groups of a shard
     int pieces, chunk, gpb, Dp;      // Dp: D to a multiple of 4, the partial sums' rows
+    int threads;                     // of a row
     long long blocks_shard, blocks;
 };
 
@@ -309,23 +353,24 @@ static NormDeal norm_deal(const BlockNorm& b, int R, bool al)
     q.Dp = (b.D + 3) / 4 * 4;
     q.group = b.gate_rows ? b.gate_rows : nb;
     q.groups_shard = q.group ? nb / q.group : 0;
+    const int w = b.dt == DT_F32 || b.layer || !al ? 4 : 8;
+    q.threads = row_threads(b.D, w, wave_reach(b, std::max<long long>(1, q.group)));
+    const int slots_block = q.threads < 256 ? 256 / q.threads : 1;
     // At most the blocks that 256 compute units hold at 16 waves each (the kernels' registers):
     // one more would run alone.  Fewer rows to a block than that gives only cost partial sums.
-    const int w = b.dt == DT_F32 || b.layer || !al ? 4 : 8;
-    int threads = 256;
-    while (threads < 1024 && threads * w < b.D) threads *= 2;
-    const long long slots = 256LL * 1024 / threads;
+    const long long slots = 256LL * 1024 / std::max(256, q.threads);
     for (long long rows = std::max<long long>(1, nb * R / slots);; rows += std::max<long long>(1, rows / 16)) {
         q.gpb = q.pieces = 1;
+        q.chunk = (int)q.group;
         if (q.group > rows) {
             q.pieces = (int)((q.group + rows - 1) / rows);
             q.chunk = (int)((q.group + q.pieces - 1) / q.pieces);
-            q.blocks_shard = q.groups_shard * q.pieces;
-        } else {
-            q.gpb = (int)(q.group ? std::max<long long>(1, rows / q.group) : 1);
-            q.chunk = (int)q.group;
-            q.blocks_shard = (q.groups_shard + q.gpb - 1) / q.gpb;
+        } else if (q.group && q.groups_shard > 1) {
+            // several groups, one to a slot at a time; fewer than slots: a block for each
+            const long long g = rows / q.group / slots_block * slots_block;
+            q.gpb = (int)std::max<long long>(1, std::min(g, q.groups_shard));
         }
+        q.blocks_shard = q.pieces > 1 ? q.groups_shard * q.pieces : (q.groups_shard + q.gpb - 1) / q.gpb;
         if (q.blocks_shard * R <= slots || rows >= nb) break;
     }
     q.blocks = q.blocks_shard * R;
@@ -351,17 +396,24 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
     __shared__ float comb[RPB > 1 ? RPB - 1 : 1][RPB > 1 ? N * NT : 1];
     int slot = 0;
     const int l = threadIdx.x % NT, D = b.D;
-    const int rs = __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
+    const Slot sl = row_slot<NT>();
+    const int rs = sl.first + sl.sub;
     const float inv_d = 1.0f / (float)D;
     const long long shard = blockIdx.x / q.blocks_shard, bs = blockIdx.x % q.blocks_shard;
     const long long nb = q.group * q.groups_shard;
-    // the block's groups, and its rows within each (runs of rows; interleaved ones took the same time)
+    // MANY: groups g0 .. g1 - 1 of the shard, one to a slot at a time.  Else a run of the rows of group g0
+    // (interleaved rows took the same time), one to a slot.
     const long long g0 = MANY ? bs * q.gpb : bs / q.pieces;
     const long long g1 = MANY ? min(g0 + q.gpb, q.groups_shard) : q.groups_shard;
     // (one group is a loop as well: with the compiler seeing a single pass, 8850 x 771 fp32 took 48 us, so 44)
-    const long long gstep = MANY ? 1 : q.groups_shard;
+    const long long gstep = MANY ? RPB : q.groups_shard;
     const int first = MANY ? 0 : (int)(bs % q.pieces) * q.chunk;
-    const int rows = (int)max(0LL, min((long long)q.chunk, q.group - first));
+    const int rows = MANY ? (int)q.group : (int)max(0LL, min((long long)q.chunk, q.group - first));
+    constexpr int rstep = MANY ? 1 : RPB;
+    // distance of a lane's rows from the first of its wave
+    const long long apart = MANY ? q.group : 1;
+    const int oh = sl.sub * (int)(apart * b.ld_h), ox = sl.sub * (int)(apart * b.ld_x),
+              oy = sl.sub * (int)(apart * b.ld_y), og = MANY && b.gate_rows ? sl.sub * D : 0;
     const bool has_x = g.x != nullptr, has_y = g.dy != nullptr;
     const bool post = b.post_w != nullptr;
     float pw[N], t1[N], pb[LAYER ? N : 1], t0[LAYER ? N : 1];
@@ -392,32 +444,39 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
     auto put = [&](int plane, const float (&v)[N]) {
         if (rs == 0) store_row<float, NT, W, C, AL>(out + (long long)plane * q.Dp, l, D, v);
     };
-    // (a slot past the rows: as wide as nothing, read and written)
-    auto row_of = [&](long long gi, int j0) {
-        return shard * nb + gi * q.group + first + (j0 + rs < rows ? j0 + rs : 0);
+    // the first row of the wave; a slot past the rows (the groups) is as wide as nothing
+    auto row_of = [&](long long gi, int j) {
+        return shard * nb + (MANY ? (gi + sl.first) * q.group + j
+                                  : gi * q.group + first + j + sl.first);
     };
-    auto width = [&](int j0) { return j0 + rs < rows ? D : 0; };
+    auto width = [&](long long gi, int j) {
+        return (MANY ? gi + rs < g1 : j + rs < rows) ? D : 0;
+    };
     Raw<T, N, AL> rH, ry;
-    auto load_y = [&](long long gi, int j0) {
-        const long long i = row_of(gi, j0);
-        load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.dy) + i * b.ld_y, l, width(j0), ry);
-        load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.h_out) + i * b.ld_h, l, width(j0), rH);
+    auto load_y = [&](long long gi, int j) {
+        const long long i = row_of(gi, j);
+        const int Dl = width(gi, j);
+        load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.dy) + i * b.ld_y, l, Dl, ry, oy);
+        load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.h_out) + i * b.ld_h, l, Dl, rH, oh);
     };
     if (has_y && rows && g0 < g1) load_y(g0, 0);
     for (long long gi = g0; gi < g1; gi += gstep) {
-        const long long base = shard * nb + gi * q.group;
-        const float* gate = b.gate ? b.gate + (b.gate_rows ? base / b.gate_rows : 0) * D : nullptr;
-        for (int j0 = 0; j0 < rows; j0 += RPB) {
-            const bool live = j0 + rs < rows;
+        // (the wave's first group)
+        const long long gate_row = b.gate_rows ? shard * q.groups_shard + gi + (MANY ? sl.first : 0) : 0;
+        const float* gate = b.gate ? b.gate + gate_row * D : nullptr;
+        const bool live_group = !MANY || gi + rs < g1;
+        for (int j0 = 0; j0 < rows; j0 += rstep) {
             const long long i = row_of(gi, j0);
-            const int Dl = width(j0);
+            const int Dl = width(gi, j0);
+            const bool live = Dl != 0;
             Raw<T, N, AL> ro, rx;
             Raw<float, N, AL> rw;
             float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (g.stats) st = *reinterpret_cast<const float4*>(g.stats + 4 * i);
+            if (g.stats && live)
+                st = *reinterpret_cast<const float4*>(g.stats + 4 * (i + sl.sub * apart));
             if (g.dh_out)
-                load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.dh_out) + i * b.ld_h, l, Dl, ro);
-            if (has_x) load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.x) + i * b.ld_x, l, Dl, rx);
+                load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.dh_out) + i * b.ld_h, l, Dl, ro, oh);
+            if (has_x) load_raw<T, NT, W, C, AL>(static_cast<const T*>(g.x) + i * b.ld_x, l, Dl, rx, ox);
             // the row's loads are issued here, not moved behind the sums
             __builtin_amdgcn_sched_barrier(0);
             float dH[N];
@@ -451,14 +510,14 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
                     float v[N];
 #pragma unroll
                     for (int k = 0; k < N; ++k) v[k] = raw_at(rH, k) > 0.f ? dH[k] : 0.f;
-                    store_row<T, NT, W, C, AL>(static_cast<T*>(g.dh) + i * b.ld_h, l, Dl, v);
+                    store_row<T, NT, W, C, AL>(static_cast<T*>(g.dh) + i * b.ld_h, l, Dl, v, oh);
                 } else {
-                    store_row<T, NT, W, C, AL>(static_cast<T*>(g.dh) + i * b.ld_h, l, Dl, dH);
+                    store_row<T, NT, W, C, AL>(static_cast<T*>(g.dh) + i * b.ld_h, l, Dl, dH, oh);
                 }
             }
             if (has_y) {
-                if (j0 + RPB < rows) load_y(gi, j0 + RPB);
-                else if (MANY && gi + 1 < g1) load_y(gi + 1, 0);
+                if (j0 + rstep < rows) load_y(gi, j0 + rstep);
+                else if (MANY && gi + gstep < g1) load_y(gi + gstep, 0);
             }
             if (!has_x) continue;
             if (live) {
@@ -474,7 +533,7 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
             // dH becomes du = scale gate dH, then dx
             if (gate) {
                 Raw<float, N, AL> rg;
-                load_raw<float, NT, W, C, AL>(gate, l, D, rg);
+                load_raw<float, NT, W, C, AL>(gate, l, Dl, rg, og);
 #pragma unroll
                 for (int k = 0; k < N; ++k) dH[k] *= b.scale * raw_at(rg, k);
             } else {
@@ -496,12 +555,14 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
                 for (int k = 0; k < N; ++k)
                     dH[k] = st.y * (dH[k] - c0 - (raw_at(rx, k) - st.x) * st.y * c1);
             }
-            store_row<T, NT, W, C, AL>(static_cast<T*>(g.dx) + i * b.ld_x, l, Dl, dH);
+            store_row<T, NT, W, C, AL>(static_cast<T*>(g.dx) + i * b.ld_x, l, Dl, dH, ox);
         }
         // the group's sums on x's side
         if (!g.gate && !g.post_w && !g.post_b) continue;
-        combine(t1);
-        if constexpr (LAYER) combine(t0);
+        if constexpr (!MANY) {
+            combine(t1);
+            if constexpr (LAYER) combine(t0);
+        }
         float v[N];
         if (g.gate) {
             Raw<float, N, AL> rw, rb;
@@ -514,16 +575,16 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
                     if (b.post_b) v[k] = fmaf(raw_at(rb, k), t0[k], v[k]);
                 v[k] *= b.scale;
             }
-            if (b.gate_rows && q.pieces == 1) {   // the whole group was here
-                if (rs == 0)
-                    store_row<float, NT, W, C, AL>(g.gate + (base / b.gate_rows) * D, l, D, v);
+            if (MANY || (b.gate_rows && q.pieces == 1)) {   // the whole group was here
+                store_row<float, NT, W, C, AL>(g.gate + gate_row * D, l,
+                                               MANY ? (live_group ? D : 0) : rs ? 0 : D, v, og);
             } else {
                 put(PL_GATE, v);
             }
         }
         if (g.post_w || g.post_b) {
             Raw<float, N, AL> rg;
-            if (gate) load_raw<float, NT, W, C, AL>(gate, l, D, rg);
+            if (gate) load_raw<float, NT, W, C, AL>(gate, l, live_group ? D : 0, rg, og);
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 const float f = gate ? b.scale * raw_at(rg, k) : b.scale;
@@ -548,7 +609,10 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
         put(PL_PRE_W, pw);
     }
     if constexpr (MANY) {
-        if (g.post_w) put(PL_POST_W, qw);
+        if (g.post_w) {
+            combine(qw);
+            put(PL_POST_W, qw);
+        }
     } else {
         if (g.post_w) put(PL_POST_W, t1);
     }
@@ -558,7 +622,10 @@ __global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(
             put(PL_PRE_B, pb);
         }
         if constexpr (MANY) {
-            if (g.post_b) put(PL_POST_B, qb);
+            if (g.post_b) {
+                combine(qb);
+                put(PL_POST_B, qb);
+            }
         } else {
             if (g.post_b) put(PL_POST_B, t0);
         }
@@ -639,7 +706,7 @@ hipError_t block_norm_bwd(const BlockNorm& b, int R, const BlockNormGrads& g, vo
             using T = decltype(t);
             constexpr bool LAYER = decltype(layer)::value, AL = decltype(aligned)::value;
             constexpr int W = kRun<T, LAYER, AL>;
-            with_row_shape<W>(b.D, [&](auto nt, auto c) {
+            with_row_shape<W>(b.D, q.threads, [&](auto nt, auto c) {
                 constexpr int NT = decltype(nt)::value, C = decltype(c)::value;
                 if (q.gpb > 1)
                     hipLaunchKernelGGL((norm_bwd_kernel<T, W, NT, C, AL, LAYER, true>),

@@ -50,7 +50,9 @@ DIMS = [  # rows, D, shards, rows of a gate (0: one gate), extra strides, offset
     (6, 65, 2, 3, 0, 0), (70, 300, 2, 7, 4, 0), (33, 771, 3, 11, 5, 1), (260, 128, 4, 65, 8, 0),
     (12, 1024, 1, 0, 0, 0), (130, 2056, 2, 5, 0, 0), (9, 4096, 3, 0, 8, 0), (5, 5001, 1, 0, 0, 0),
     (4, 8192, 2, 1, 0, 0), (3, 16384, 1, 0, 0, 0), (2, 16383, 1, 2, 1, 1), (1100, 40, 2, 0, 0, 0),
-    (4097, 16, 1, 0, 0, 0), (520, 513, 1, 520, 0, 0)]
+    (4097, 16, 1, 0, 0, 0), (520, 513, 1, 520, 0, 0), (1200, 64, 3, 2, 0, 0), (999, 100, 3, 3, 4, 1),
+    (2048, 128, 2, 16, 0, 0), (4100, 24, 4, 1, 0, 0), (300, 200, 2, 5, 8, 0), (5001, 96, 1, 0, 0, 0),
+    (2310, 252, 2, 33, 4, 0), (7000, 8, 2, 7, 0, 0)]
 FORMS = [  # layer norm, post norm, gate, x
     (False, True, True, True), (True, True, True, True), (False, True, False, True),
     (True, False, True, True), (False, False, False, True), (True, False, False, False),
