@@ -160,6 +160,7 @@ __device__ __forceinline__ void row_sum(float (&v)[M], float (&red)[2][M][16], i
 }
 
 constexpr int block_of(int NT) { return NT < 256 ? 256 : NT; }
+constexpr int bwd_block(int NT) { return NT < 512 ? 512 : NT; }
 
 // A block holds block_of(NT) / NT rows at a time, one to a slot.  first: the wave's first slot (the same
 // in all its lanes); sub: the lane's slot after it.
@@ -355,10 +356,10 @@ static NormDeal norm_deal(const BlockNorm& b, int R, bool al)
     q.groups_shard = q.group ? nb / q.group : 0;
     const int w = b.dt == DT_F32 || b.layer || !al ? 4 : 8;
     q.threads = row_threads(b.D, w, wave_reach(b, std::max<long long>(1, q.group)));
-    const int slots_block = q.threads < 256 ? 256 / q.threads : 1;
+    const int slots_block = q.threads < 512 ? 512 / q.threads : 1;
     // At most the blocks that 256 compute units hold at 16 waves each (the kernels' registers):
     // one more would run alone.  Fewer rows to a block than that gives only cost partial sums.
-    const long long slots = 256LL * 1024 / std::max(256, q.threads);
+    const long long slots = 256LL * 1024 / std::max(512, q.threads);
     for (long long rows = std::max<long long>(1, nb * R / slots);; rows += std::max<long long>(1, rows / 16)) {
         q.gpb = q.pieces = 1;
         q.chunk = (int)q.group;
@@ -388,10 +389,10 @@ enum { PL_PRE_W, PL_POST_W, PL_GATE, PL_PRE_B, PL_POST_B, kPlanes };
 // 47 -> 44 us).  8192 x 4096 bf16, four shards: 97 us, 4.4 TB/s with the partial sums; half the
 // blocks 128, twice as many 100.
 template <typename T, int W, int NT, int C, bool AL, bool LAYER, bool MANY>
-__global__ __launch_bounds__(block_of(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(BlockNorm b, BlockNormGrads g,
+__global__ __launch_bounds__(bwd_block(NT), C == 1 ? 4 : 1) void norm_bwd_kernel(BlockNorm b, BlockNormGrads g,
                                                                 NormDeal q, float* __restrict__ part)
 {
-    constexpr int N = W * C, RPB = block_of(NT) / NT, M = LAYER ? 2 : 1;
+    constexpr int N = W * C, RPB = bwd_block(NT) / NT, M = LAYER ? 2 : 1;
     __shared__ float red[2][M][16];
     __shared__ float comb[RPB > 1 ? RPB - 1 : 1][RPB > 1 ? N * NT : 1];
     int slot = 0;
@@ -710,10 +711,10 @@ hipError_t block_norm_bwd(const BlockNorm& b, int R, const BlockNormGrads& g, vo
                 constexpr int NT = decltype(nt)::value, C = decltype(c)::value;
                 if (q.gpb > 1)
                     hipLaunchKernelGGL((norm_bwd_kernel<T, W, NT, C, AL, LAYER, true>),
-                                       dim3((unsigned)q.blocks), dim3(block_of(NT)), 0, s, b, g, q, part);
+                                       dim3((unsigned)q.blocks), dim3(bwd_block(NT)), 0, s, b, g, q, part);
                 else
                     hipLaunchKernelGGL((norm_bwd_kernel<T, W, NT, C, AL, LAYER, false>),
-                                       dim3((unsigned)q.blocks), dim3(block_of(NT)), 0, s, b, g, q, part);
+                                       dim3((unsigned)q.blocks), dim3(bwd_block(NT)), 0, s, b, g, q, part);
             });
         };
         with_form(b, al, go);
