@@ -249,10 +249,8 @@ __global__ __launch_bounds__(block_of(NT)) void norm_fwd_kernel(BlockNorm b, con
 
 static bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// Elements of a run: 16 bytes, or 8 of bf16 where a backward thread with 8 would not fit the 128
-// registers of two blocks to a compute unit (the biases' sums of a layer norm, single elements).
-template <typename T, bool LAYER, bool AL>
-constexpr int kRun = sizeof(T) == 4 || LAYER || !AL ? 4 : 8;
+// Elements of a run: 16 bytes; four where they are loaded singly.
+template <typename T, bool AL> constexpr int kRun = sizeof(T) == 4 || !AL ? 4 : 8;
 
 // Calls go(type, layer norm, aligned) as constants.
 template <class F> static void with_form(const BlockNorm& b, bool al, F go)
@@ -313,7 +311,7 @@ hipError_t block_norm_fwd(const BlockNorm& b, const void* h, const void* x, void
     auto go = [&](auto t, auto layer, auto aligned) {
         using T = decltype(t);
         constexpr bool LAYER = decltype(layer)::value, AL = decltype(aligned)::value;
-        constexpr int W = kRun<T, LAYER, AL>;
+        constexpr int W = kRun<T, AL>;
         with_row_shape<W>(b.D, row_threads(b.D, W, wave_reach(b, 1)), [&](auto nt, auto c) {
             constexpr int NT = decltype(nt)::value, C = decltype(c)::value;
             constexpr int RPB = block_of(NT) / NT;
@@ -343,18 +341,18 @@ hipError_t block_norm_fwd(const BlockNorm& b, const void* h, const void* x, void
 struct NormDeal {
     long long group, groups_shard;   // rows of a group, groups of a shard
     int pieces, chunk, gpb, Dp;      // Dp: D to a multiple of 4, the partial sums' rows
-    int threads;                     // of a row
+    int threads, run;                // of a row; elements of a thread's run
     long long blocks_shard, blocks;
 };
 
-static NormDeal norm_deal(const BlockNorm& b, int R, bool al)
+static NormDeal norm_deal_runs(const BlockNorm& b, int R, int w)
 {
     NormDeal q{};
+    q.run = w;
     const long long nb = b.rows / R;
     q.Dp = (b.D + 3) / 4 * 4;
     q.group = b.gate_rows ? b.gate_rows : nb;
     q.groups_shard = q.group ? nb / q.group : 0;
-    const int w = b.dt == DT_F32 || b.layer || !al ? 4 : 8;
     q.threads = row_threads(b.D, w, wave_reach(b, std::max<long long>(1, q.group)));
     const int slots_block = q.threads < 512 ? 512 / q.threads : 1;
     // At most the blocks that 256 compute units hold at 16 waves each (the kernels' registers):
@@ -376,6 +374,14 @@ static NormDeal norm_deal(const BlockNorm& b, int R, bool al)
     }
     q.blocks = q.blocks_shard * R;
     return q;
+}
+
+// A block of several groups with the biases' sums has no registers for runs of 8 (65536 x 128 bf16, gates
+// of 2 rows: 73 us, with runs of 4 44; a block of one group: 32768 x 512 54 and 72).
+static NormDeal norm_deal(const BlockNorm& b, int R, bool al)
+{
+    const NormDeal q = norm_deal_runs(b, R, b.dt == DT_F32 || !al ? 4 : 8);
+    return q.run == 8 && q.gpb > 1 && b.layer ? norm_deal_runs(b, R, 4) : q;
 }
 
 // planes of a block's partial sums
@@ -706,16 +712,26 @@ hipError_t block_norm_bwd(const BlockNorm& b, int R, const BlockNormGrads& g, vo
         auto go = [&](auto t, auto layer, auto aligned) {
             using T = decltype(t);
             constexpr bool LAYER = decltype(layer)::value, AL = decltype(aligned)::value;
-            constexpr int W = kRun<T, LAYER, AL>;
-            with_row_shape<W>(b.D, q.threads, [&](auto nt, auto c) {
-                constexpr int NT = decltype(nt)::value, C = decltype(c)::value;
-                if (q.gpb > 1)
-                    hipLaunchKernelGGL((norm_bwd_kernel<T, W, NT, C, AL, LAYER, true>),
-                                       dim3((unsigned)q.blocks), dim3(bwd_block(NT)), 0, s, b, g, q, part);
-                else
-                    hipLaunchKernelGGL((norm_bwd_kernel<T, W, NT, C, AL, LAYER, false>),
-                                       dim3((unsigned)q.blocks), dim3(bwd_block(NT)), 0, s, b, g, q, part);
-            });
+            auto launch = [&](auto w, auto many) {
+                constexpr int W = decltype(w)::value;
+                constexpr bool MANY = decltype(many)::value;
+                with_row_shape<W>(b.D, q.threads, [&](auto nt, auto c) {
+                    constexpr int NT = decltype(nt)::value, C = decltype(c)::value;
+                    hipLaunchKernelGGL((norm_bwd_kernel<T, W, NT, C, AL, LAYER, MANY>),
+                                       dim3((unsigned)q.blocks), dim3(bwd_block(NT)), 0, s, b, g, q,
+                                       part);
+                });
+            };
+            const std::integral_constant<int, 4> four;
+            const std::integral_constant<int, kRun<T, AL>> full;
+            if constexpr (kRun<T, AL> == 8 && LAYER) {
+                if (q.gpb > 1) launch(four, std::true_type());
+                else if (q.run == 4) launch(four, std::false_type());
+                else launch(full, std::false_type());
+            } else {
+                if (q.gpb > 1) launch(full, std::true_type());
+                else launch(full, std::false_type());
+            }
         };
         with_form(b, al, go);
         const hipError_t e = hipGetLastError();
