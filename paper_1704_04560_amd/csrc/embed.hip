@@ -517,10 +517,13 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGather a)
     put_row<1, false, 1>(a, r, t, c, v);
 }
 
-// Few tokens (n <= kSmallTokens) take one launch: a block sorts the tokens of its rows into LDS, and
-// its waves add them, a row each; rows with more than 32 terms are added by all waves, which take
-// equal runs of the terms.  n = 257 x 4 shards, 5003 rows of 300: three launches 19.8 us, one 13.4.
-constexpr int kSmallTokens = 1024;
+// Few tokens (n <= kSmallTokens, at most kSmallValues of dy) take one launch: a block sorts the tokens of
+// its rows into LDS, and its waves add them, a row each; rows with more than 32 terms are added by
+// all waves, which take equal runs of the terms.  4 x 257 tokens, 5003 rows of 300: 19.8 us in three
+// launches, 13 in one; 256 x 1024 added to what is there 17 and 10.  Past the limits a wave's rows one
+// after the other take longer than the launches: 1000 x 300 18 and 27, 256 x 4096 17 and 22.
+constexpr int kSmallTokens = 512;
+constexpr long long kSmallValues = 1 << 19;
 template <typename T, int E, bool VEC>
 __global__ __launch_bounds__(64 * kIndexWaves) void embed_small_kernel(EmbedIndex x, EmbedGather a)
 {
@@ -691,7 +694,7 @@ hipError_t embed_bwd(const int* tok, long long n, int R, const void* dy, Dt dt, 
     a.scale = scale; a.grads = grads; a.ld = ld; a.accumulate = accumulate;
     a.part = reinterpret_cast<float*>(base + q.part);
     a.Dp = q.Dp;
-    if (n <= kSmallTokens) {
+    if (n <= kSmallTokens && R * n * D <= kSmallValues) {
         if (dt == DT_F32 && vec)
             hipLaunchKernelGGL((embed_small_kernel<float, 4, true>), grid, block, lds, s, x, a);
         else if (dt == DT_F32)
