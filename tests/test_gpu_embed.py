@@ -67,6 +67,8 @@ CASES = [  # V, D, n, R, pad, scale, token law, extra lddy, offset, extra ld
     (3, 1, 9000, 1, 2, 1.0, "uniform", 0, 0, 0), (600, 256, 128, 8, -1, 1.0, "two", 0, 0, 0),
     (500, 200, 3001, 2, 0, 1.0, "zipf", 0, 0, 4), (300, 1032, 2500, 1, -1, 0.5, "zipf", 8, 0, 0),
     (900, 264, 1025, 3, -1, 1.0, "uniform", 0, 0, 0), (50, 16, 70000, 1, -1, 1.0, "one", 0, 0, 0),
+    (3, 64, 500, 1, -1, 1.0, "uniform", 0, 0, 0), (9, 200, 512, 2, 4, 1.0, "one", 0, 0, 0),
+    (40, 130, 400, 2, -1, 1.0, "two", 0, 0, 0), (9, 200, 512, 1, -1, 1.0, "one", 8, 0, 0),
     (131072, 16, 300, 1, -1, 1.0, "zipf", 0, 0, 0), (1 << 20, 8, 2100, 1, 5, 1.0, "zipf", 0, 0, 0),
     (30, 128, 6000, 2, 29, 1.0, "two", 0, 0, 0), (40, 2056, 1024, 1, -1, 1.0, "one", 0, 0, 0),
 ]
