@@ -353,7 +353,8 @@ static NormDeal norm_deal_runs(const BlockNorm& b, int R, int w)
     q.Dp = (b.D + 3) / 4 * 4;
     q.group = b.gate_rows ? b.gate_rows : nb;
     q.groups_shard = q.group ? nb / q.group : 0;
-    q.threads = row_threads(b.D, w, wave_reach(b, std::max<long long>(1, q.group)));
+    // (rows that share a wave: neighbours, or of neighbouring gate groups)
+    q.threads = row_threads(b.D, w, wave_reach(b, b.gate_rows ? b.gate_rows : 1));
     const int slots_block = q.threads < 512 ? 512 / q.threads : 1;
     // At most the blocks that 256 compute units hold at 16 waves each (the kernels' registers):
     // one more would run alone.  Fewer rows to a block than that gives only cost partial sums.

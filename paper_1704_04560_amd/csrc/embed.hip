@@ -314,7 +314,7 @@ struct EmbedGather {
     int Dp;
 };
 
-// E values of a row of dy or of fp32: 16-byte vectors (VEC), else single elements 64 apart.
+// E values of a row of dy or of fp32: 16-byte vectors (VEC), else single elements L apart.
 template <typename T, int E, bool VEC, int L>
 __device__ __forceinline__ void load_row(const T* p, int c, int D, float (&v)[E])
 {
@@ -364,16 +364,16 @@ __device__ __forceinline__ void put_row(const EmbedGather& a, int r, int t, int 
     store_row<E, VEC, L>(out, c, a.D, v);
 }
 
-// A block takes G = 512 / L pieces of P positions in a row and E L columns, a group of L lanes one
-// piece, U rows of dy in flight at a time.  A row of the table whose terms all lie in one group's
+// A block takes kGroups pieces of P positions in a row and E L columns, a group of L lanes one piece,
+// U rows of dy in flight at a time.  A row of the table whose terms all lie in one group's
 // piece is written by the group; the sums at a group's edges meet in LDS, where they are joined in
 // order; what reaches over the block's edges becomes a partial sum of the block: slot 0 the
 // row that began in an earlier block, slot 1 one that begins here and goes on.
-constexpr int kGatherThreads = 512;
+constexpr int kGroups = 8;
 template <typename T, int E, bool VEC, int L>
-__global__ __launch_bounds__(kGatherThreads) void embed_gather_kernel(EmbedGather a)
+__global__ __launch_bounds__(kGroups * L) void embed_gather_kernel(EmbedGather a)
 {
-    constexpr int U = 8, G = kGatherThreads / L, W = E * L;
+    constexpr int U = 8, G = kGroups, W = E * L;
     // per group: the sum of a row that began earlier (head), and of one that goes on (tail)
     __shared__ float edge[G][2][W];
     __shared__ int edge_row[G][2];   // their rows, -1: none
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(kGatherThreads) void embed_gather_kernel(EmbedGathe
         flush(goes_on);
     }
     __syncthreads();
-    for (int q = threadIdx.x; q < W; q += kGatherThreads) {
+    for (int q = threadIdx.x; q < W; q += kGroups * L) {
         const int col = slice * W + q;
         if (col >= a.D) break;
         float* part = a.part + pc * 2 * a.Dp + col;
@@ -625,7 +625,7 @@ static EmbedPlan embed_plan(long long n, int R, int V, int D)
     q.row = take(N * 4);
     q.span = take(((size_t)R << q.lg) * q.bins * sizeof(RowSpan));
     q.valid = take((size_t)R * 4);
-    const size_t most = (n + kGatherThreads / 64 * kMinP - 1) / (kGatherThreads / 64 * kMinP);
+    const size_t most = (n + kGroups * kMinP - 1) / (kGroups * kMinP);
     q.part = take(most > 1 ? (size_t)R * most * 2 * q.Dp * 4 : 0);
     return q;
 }
@@ -635,7 +635,7 @@ size_t embed_bwd_bytes(long long n, int R, int V, int D) { return embed_plan(n, 
 template <typename T, int E, bool VEC, int L>
 static hipError_t launch_gather(EmbedGather a, hipStream_t s)
 {
-    constexpr int G = kGatherThreads / L;
+    constexpr int G = kGroups;
     a.slices = (a.D + E * L - 1) / (E * L);
     // the longest piece that still gives two blocks for every compute unit
     for (a.P = kMaxP; a.P > kMinP; a.P /= 2)
@@ -644,7 +644,7 @@ static hipError_t launch_gather(EmbedGather a, hipStream_t s)
     a.pieces = (a.n + a.BP - 1) / a.BP;
     const long long pieces = (long long)a.R * a.pieces;
     hipLaunchKernelGGL((embed_gather_kernel<T, E, VEC, L>), dim3((unsigned)(pieces * a.slices)),
-                       dim3(kGatherThreads), 0, s, a);
+                       dim3(kGroups * L), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.pieces <= 1) return e;
     timing_split(s, "join");
