@@ -147,12 +147,13 @@ constexpr int kIndexBins = 512;   // rows of a bucket: 16 x 512 counters are 32 
 // number of tokens in lower buckets, counted on the way, is where the block's part begins:
 // blocks do not wait for one another.
 struct BlockSort {
-    static constexpr int K = 16;
+    static constexpr int K = 32;
     const int* tok;
     int* hist;             // LDS [kIndexWaves][bins] counters, then [bins] totals of the rows
     int *red, *red2;       // LDS [kIndexWaves]
     int i0, i1, base, all, NB, b, lane, w;
     int t[K];              // the wave's last (or only) loads
+    unsigned hit;          // which of them hold a token of the block
 
     __device__ __forceinline__ bool mine(const EmbedIndex& a, int v) const
     {
@@ -161,7 +162,10 @@ struct BlockSort {
     __device__ __forceinline__ void load(int i)
     {
 #pragma unroll
-        for (int k = 0; k < K; ++k) t[k] = i + k * 64 + lane < i1 ? tok[i + k * 64 + lane] : -1;
+        for (int k = 0; k < K; ++k) {
+            if (i + k * 64 >= i1) break;
+            t[k] = i + k * 64 + lane < i1 ? tok[i + k * 64 + lane] : -1;
+        }
     }
     // Count; on return hist holds positions, and thread q < bins the first one (pos) and the
     // number (total) of its row's tokens.
@@ -170,21 +174,27 @@ struct BlockSort {
         const int tid = threadIdx.x;
         for (int i = tid; i < kIndexWaves * a.bins; i += 64 * kIndexWaves) hist[i] = 0;
         __syncthreads();
-        const int per = (a.n / (64 * kIndexWaves) + 1) * 64;
+        const int per = (a.n + 64 * kIndexWaves - 1) / (64 * kIndexWaves) * 64;
         i0 = min((long long)w * per, (long long)a.n);
         i1 = min((long long)i0 + per, (long long)a.n);
         int lower = 0;
+        hit = 0;
         for (int i = i0; i < i1; i += 64 * K) {
             load(i);
+            hit = 0;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
+                if (i + k * 64 >= i1) break;
                 const bool ok = (unsigned)t[k] < (unsigned)a.V && t[k] != a.pad;
-                if (ok && (t[k] & (NB - 1)) < b) ++lower;
-                if (mine(a, t[k])) atomicAdd(&hist[w * a.bins + (t[k] >> a.lg)], 1);
+                const int m = ok ? t[k] & (NB - 1) : NB;
+                lower += __popcll(__ballot(m < b));
+                // (most of them hold no token of the block: a branch of the whole wave)
+                if (__ballot(m == b)) {
+                    hit |= 1u << k;
+                    if (m == b) atomicAdd(&hist[w * a.bins + (t[k] >> a.lg)], 1);
+                }
             }
         }
-#pragma unroll
-        for (int o = 32; o; o >>= 1) lower += __shfl_xor(lower, o);
         if (lane == 0) red[w] = lower;
         __syncthreads();
         // exclusive scan of the rows' totals; a thread takes one row (bins <= 512)
@@ -226,9 +236,14 @@ struct BlockSort {
     {
         int* at_row = hist + w * a.bins;
         for (int i = i0; i < i1; i += 64 * K) {
-            if (i1 - i0 > 64 * K) load(i);
+            if (i1 - i0 > 64 * K) {
+                load(i);
+                hit = ~0u;
+            }
 #pragma unroll
             for (int k = 0; k < K; ++k) {
+                if (i + k * 64 >= i1) break;
+                if (!(hit >> k & 1)) continue;
                 const bool ok = mine(a, t[k]);
                 unsigned long long left = __ballot(ok);
                 // the rows met among these 64 tokens, one after the other
@@ -520,7 +535,7 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedGather a)
 // Few tokens (n <= kSmallTokens, at most kSmallValues of dy) take one launch: a block sorts the tokens of
 // its rows into LDS, and its waves add them, a row each; rows with more than 32 terms are added by
 // all waves, which take equal runs of the terms.  4 x 257 tokens, 5003 rows of 300: 19.8 us in three
-// launches, 13 in one; 256 x 1024 added to what is there 17 and 10.  Past the limits a wave's rows one
+// launches, 11.5 in one; 256 x 1024 added to what is there 17 and 10.  Past the limits a wave's rows one
 // after the other take longer than the launches: 1000 x 300 18 and 27, 256 x 4096 17 and 22.
 constexpr int kSmallTokens = 512;
 constexpr long long kSmallValues = 1 << 19;
