@@ -430,7 +430,8 @@ int mtx_embed_backward(const int32_t* tokens, size_t n, int R, const void* dy, i
  *                  sequence's gate); must divide the rows of a shard.
  * Weights and gates are fp32.  ld_h, ld_x, ld_y: strides between rows (0: D) of h and h_out (and
  * dh, dh_out), of x (dx), of y (dy).  1 <= D <= 16384, rows < 2^31 (rows = 0 does nothing),
- * eps >= 0 (a row of zeros with eps = 0 gives NaN). */
+ * eps >= 0 (a row of zeros with eps = 0 gives NaN).  Squares are fp32: a row whose mean square is
+ * beyond its range gives 0 or NaN. */
 typedef enum { MTX_NORM_RMS = 0, MTX_NORM_LAYER = 1 } mtx_norm_kind;
 typedef struct {
     int kind;     /* mtx_norm_kind */

@@ -28,8 +28,9 @@ struct ClipOut {
     int* nonfinite;
 };
 
-// Every block: the norm from the partial sums, and the factor.
-__device__ __forceinline__ float clip_factor(const double* part, int np, const ClipOut& o)
+// Every block: the norm from the partial sums, and the factor (a double: max_norm / norm may be below
+// fp32's range where its products are not).
+__device__ __forceinline__ double clip_factor(const double* part, int np, const ClipOut& o)
 {
     __shared__ double red[4];
     double v = 0.0;
@@ -40,7 +41,7 @@ __device__ __forceinline__ float clip_factor(const double* part, int np, const C
         if (o.norm) *o.norm = (float)norm;
         if (o.nonfinite) *o.nonfinite = fin ? 0 : 1;
     }
-    return fin && norm > (double)o.max_norm ? (float)((double)o.max_norm / norm) : 1.0f;
+    return fin && norm > (double)o.max_norm ? (double)o.max_norm / norm : 1.0;
 }
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -49,8 +50,8 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 // 16-byte vectors, two per thread and pass, 4 KB apart; the rows are read once (nontemporal).  The
 // average is read again by the second launch; it is written through the caches, or past them where
 // the rows' traffic would push it out (AVG_PAST).  The n % 4 elements left over: the grid's first
-// thread.  AVG_UNALIGNED: rows or an average that start at any element (unaligned
-// vectors: 16 x 5M 72 us, single ones 99).  16 x 61M: 697 us, 5.95 TB/s.
+// thread.  AVG_UNALIGNED: rows or an average that start at any element (16 x 5M: unaligned vectors
+// 72 us, single elements 99).  16 x 61M: 697 us, 5.95 TB/s.
 enum Avg { AVG_CACHED, AVG_PAST, AVG_UNALIGNED };
 template <int RT, bool EXACT, Avg HOW>
 __global__ __launch_bounds__(256) void avg_sq_vec4(const float* __restrict__ grads, int Rrt,
@@ -126,15 +127,21 @@ __global__ __launch_bounds__(256) void scale_kernel(float* __restrict__ g, long 
                                                     const double* __restrict__ part, int np,
                                                     ClipOut o)
 {
-    const float f = clip_factor(part, np, o);
-    if (f == 1.0f) return;
+    const double f = clip_factor(part, np, o);
+    if (f == 1.0) return;
     const long long step = (long long)gridDim.x * 256, n4 = (n - head) / 4;
     const long long t = (long long)blockIdx.x * 256 + threadIdx.x;
     f32x4* g4 = reinterpret_cast<f32x4*>(g + head);
 #pragma unroll 2
-    for (long long i = n4 - 1 - t; i >= 0; i -= step) g4[i] *= f;
-    if (t < head) g[t] *= f;
-    if (head + 4 * n4 + t < n) g[head + 4 * n4 + t] *= f;
+    for (long long i = n4 - 1 - t; i >= 0; i -= step) {
+        f32x4 v = g4[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = (float)(f * (double)v[j]);
+        g4[i] = v;
+    }
+    if (t < head) g[t] = (float)(f * (double)g[t]);
+    const long long rest = head + 4 * n4 + t;
+    if (rest < n) g[rest] = (float)(f * (double)g[rest]);
 }
 
 template <bool EXACT>
@@ -247,7 +254,7 @@ __global__ __launch_bounds__(256) void list_sq_kernel(const ClipChunk* __restric
 // caches (291 tensors bf16 -> fp32 at odd places of one vector, both launches: single elements
 // through the caches 117 us; past them 120, half-line vectors 108, whole ones 88).
 template <bool SB, bool DB>
-__device__ __forceinline__ void chunk_scale(const ClipChunk& k, float f)
+__device__ __forceinline__ void chunk_scale(const ClipChunk& k, double f)
 {
     constexpr int W = DB ? 8 : 4, U = 2;
     constexpr int SW = W * (SB ? 2 : 4) / 4;   // words of the source
@@ -281,7 +288,9 @@ __device__ __forceinline__ void chunk_scale(const ClipChunk& k, float f)
             float v[W];
 #pragma unroll
             for (int j = 0; j < W; ++j)
-                v[j] = f * __uint_as_float(!SB ? w[u][j] : j % 2 ? w[u][j / 2] & 0xffff0000u : w[u][j / 2] << 16);
+                v[j] = (float)(f * (double)__uint_as_float(!SB     ? w[u][j]
+                                                          : j % 2 ? w[u][j / 2] & 0xffff0000u
+                                                                  : w[u][j / 2] << 16));
             u32x4 r;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -291,7 +300,7 @@ __device__ __forceinline__ void chunk_scale(const ClipChunk& k, float f)
         }
     }
     chunk_rest(k, k.head + nv * W, [&](unsigned i) {
-        const float g = f * load_elem(k.src, SB, i);
+        const float g = (float)(f * (double)load_elem(k.src, SB, i));
         if (DB) static_cast<bf16_t*>(k.dst)[i] = f32_to_bf16(g);
         else static_cast<float*>(k.dst)[i] = g;
     });
@@ -303,11 +312,11 @@ __global__ __launch_bounds__(256) void list_scale_kernel(const ClipChunk* __rest
                                                          const double* __restrict__ part, int np,
                                                          ClipOut o)
 {
-    const float f = clip_factor(part, np, o);
-    if (all_in_place && f == 1.0f) return;
+    const double f = clip_factor(part, np, o);
+    if (all_in_place && f == 1.0) return;
     for (int c = count - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
         const ClipChunk k = chunks[c];
-        if (!k.dst || (k.dst == k.src && f == 1.0f)) continue;
+        if (!k.dst || (k.dst == k.src && f == 1.0)) continue;
         if (k.src_bf16) k.dst_bf16 ? chunk_scale<true, true>(k, f) : chunk_scale<true, false>(k, f);
         else k.dst_bf16 ? chunk_scale<false, true>(k, f) : chunk_scale<false, false>(k, f);
     }

@@ -126,17 +126,19 @@ def test_a_norm_that_is_not_finite_clips_nothing(bad):
 
 def test_large_and_tiny_values():
     """Squares beyond fp32's range on both sides still give the norm."""
-    for v in (3e30, 1e-30):
+    for v, m in ((3e30, 1.0), (1e-30, 1.0), (3e33, 1e-20)):   # (a factor below fp32's range)
         a = torch.full((1000,), v, device="cuda")
         nrm = torch.zeros(1, device="cuda")
+        avg = torch.empty(1000, device="cuda")
+        mtx.mtx_average_clip(a, 1, 1000, 1000, m, avg, nrm, _ws())
         clip = mtx.Clip([(a, a)])
-        clip.clip(1.0, nrm)
+        clip.clip(m, nrm)
         torch.cuda.synchronize()
         x = float(torch.tensor(v, dtype=F32).double())
         want = x * 1000 ** 0.5
         assert abs(nrm.item() - want) <= 2 * U * want
-        ref = min(1.0, 1.0 / want) * x
-        assert abs(a[0].item() - ref) <= 4 * U * ref
+        ref = min(1.0, float(torch.tensor(m).double()) / want) * x
+        assert abs(a[0].item() - ref) <= 4 * U * ref and torch.equal(a, avg)
 
 
 def test_zero_gradients():
@@ -184,3 +186,31 @@ def test_norm_out_inside_the_list_is_refused():
         assert e.value.code == mtx.MTX_EINVAL
     clip.clip(1.0, a[200:])
     assert abs(a[200].item() - 550 ** 0.5) <= 2 * U * 550 ** 0.5
+
+
+def test_two_graphs_of_one_handle_and_workspace():
+    """Replayed in turn, each with its own bound, over workspaces that they share."""
+    g = _gen(6)
+    n = 50_001
+    a, out, nrm = torch.zeros(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty(1, device="cuda")
+    rows, avg = torch.zeros(2, n, device="cuda"), torch.empty(n, device="cuda")
+    clip, ws = mtx.Clip([(a, out)]), _ws()
+    graphs = []
+    torch.cuda.synchronize()
+    for m in (0.5, 2.0):
+        graphs.append((m, torch.cuda.CUDAGraph()))
+        with torch.cuda.graph(graphs[-1][1]):
+            clip.clip(m, nrm)
+            mtx.mtx_average_clip(rows, 2, n, n, m, avg, None, ws)
+    for k in range(4):
+        a.copy_(torch.randn(n, generator=g))
+        rows.copy_(torch.randn(2, n, generator=g))
+        m, graph = graphs[k % 2]
+        clip.clip(m, nrm)
+        mtx.mtx_average_clip(rows, 2, n, n, m, avg, None, ws)
+        want = [t.clone() for t in (out, avg, nrm)]
+        for t in (out, avg, nrm):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(want, (out, avg, nrm)))

@@ -204,3 +204,28 @@ def test_tables_and_rows_past_32_bits():
     _bwd(big, 1200, 1, dy, D, V, D, -1, 1.0, grads, V * D, True)
     ref, mag, cnt = embed_grad((big.cpu().long() % 1009), dy.cpu(), 1009, -1, 1.0)
     assert_within(grads[rows.cuda()], ref[rows % 1009], U * (cnt + 3)[rows % 1009] * mag[rows % 1009], "rows")
+
+
+def test_two_graphs_of_one_workspace():
+    """The few-token and the sorted form, replayed in turn over the same workspace and tokens."""
+    V, D = 900, 256
+    g = _gen(12)
+    tok = torch.zeros(4000, dtype=torch.int32, device="cuda")
+    dy = torch.zeros(4000, D, device="cuda")
+    out = torch.empty(V, D, device="cuda")
+    ws = torch.empty(mtx.mtx_embed_sizes(4000, 1, V, D), dtype=torch.uint8, device="cuda")
+    graphs = []
+    torch.cuda.synchronize()
+    for n in (100, 4000):
+        graphs.append((n, torch.cuda.CUDAGraph()))
+        with torch.cuda.graph(graphs[-1][1]):
+            mtx.mtx_embed_backward(tok, n, 1, dy, mtx.MTX_F32, D, V, D, -1, 1.0, out, V * D, False, ws)
+    for k in range(4):
+        tok.copy_(torch.randint(0, V, (4000,), generator=g, dtype=torch.int32))
+        dy.copy_(torch.randn(4000, D, generator=g))
+        out.fill_(3.0)
+        n, graph = graphs[k % 2]
+        graph.replay()
+        torch.cuda.synchronize()
+        ref, mag, cnt = embed_grad(tok[:n].cpu(), dy[:n].cpu(), V, -1, 1.0)
+        assert_within(out, ref, U * (cnt + 3) * mag, "gradient")
