@@ -723,11 +723,9 @@ hipError_t block_norm_bwd(const BlockNorm& b, int R, const BlockNormGrads& g, vo
                                        part);
                 });
             };
-            const std::integral_constant<int, 4> four;
             const std::integral_constant<int, kRun<T, AL>> full;
             if constexpr (kRun<T, AL> == 8 && LAYER) {
-                if (q.gpb > 1) launch(four, std::true_type());
-                else if (q.run == 4) launch(four, std::false_type());
+                if (q.gpb > 1) launch(std::integral_constant<int, 4>(), std::true_type());
                 else launch(full, std::false_type());
             } else {
                 if (q.gpb > 1) launch(full, std::true_type());
