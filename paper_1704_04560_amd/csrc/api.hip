@@ -585,8 +585,9 @@ int plan_with(const mtx_model_desc* d, int R, int Nb, bool halo, Plan& pl)
     // A residual addition passes its output gradient to the previous layer unchanged when that
     // layer has no ReLU (its output is not read by any other addition): the previous layer then
     // reads the addition's gradient buffer itself instead of a copy (the batch normalisation
-    // before each addition of the residual networks: one tensor written and read less).
-    for (size_t i = 1; i < pl.L.size(); ++i) {
+    // before each addition of the residual networks: one tensor written and read less).  From the
+    // last layer to the first, so that additions in a row all take the last one's buffer.
+    for (size_t i = pl.L.size() - 1; i > 0; --i) {
         LayerPlan& lp = pl.L[i];
         lp.dy_shared = false;
         if ((lp.kind != MTX_ADD && lp.kind != MTX_ADDP) || !lp.need_dx || pl.L[i - 1].relu)
