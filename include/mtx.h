@@ -487,7 +487,10 @@ int mtx_average_clip(const float* grads, int R, size_t n, size_t ld, float max_n
  * place, dst = NULL only counts towards the norm.  No dst may overlap another tensor's src or
  * dst, nor norm_out any of them.  The handle keeps the list in the caller's workspace (mtx_clip_sizes bytes, 256-byte
  * aligned), which with the tensors must stay valid until mtx_free_clip; mtx_init_clip copies it
- * there and synchronises with `stream`.  A handle must not be used on two streams at once. */
+ * there and synchronises with `stream`.  A handle must not be used on two streams at once.
+ * mtx_free_clip waits for the stream of the handle's last call, which must still exist (it does not
+ * wait for one that is being captured); a graph that holds calls of the handle needs the workspace
+ * and the tensors for as long as it is replayed. */
 typedef struct {
     const void* src;
     void* dst;

@@ -1827,11 +1827,7 @@ static int train_step(mtx_model* m, const float* x, bool tokens, const int32_t* 
     if (!std::isfinite(lr) || !std::isfinite(momentum))
         return fail(MTX_EINVAL, "lr and momentum must be finite");
     hipStream_t s = static_cast<hipStream_t>(stream);
-    GraphCache& gc = m->graph;
-    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-    const bool caller_capturing =
-        hipStreamIsCapturing(s, &cap) == hipSuccess && cap != hipStreamCaptureStatusNone;
-    (void)hipGetLastError();
+    const bool caller_capturing = being_captured(s);
     if (m->check_finite && (m->opt != MTX_OPT_MOMENTUM || caller_capturing))
         return fail(MTX_EUNSUPPORTED, "the non-finite check needs the momentum rule and a stream "
                                       "that is not being captured");

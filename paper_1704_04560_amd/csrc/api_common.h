@@ -32,4 +32,20 @@ inline bool overlap(const void* a, size_t abytes, const void* b, size_t bbytes)
     return x < y + bbytes && y < x + abytes;
 }
 
+inline bool being_captured(hipStream_t s)
+{
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    const bool yes = hipStreamIsCapturing(s, &cap) == hipSuccess && cap != hipStreamCaptureStatusNone;
+    (void)hipGetLastError();
+    return yes;
+}
+
+// Wait for what was enqueued on a stream.  Calls on a stream that is being captured have not run,
+// and waiting for them would end the capture.
+inline void finish_stream(hipStream_t s)
+{
+    if (!being_captured(s)) (void)hipStreamSynchronize(s);
+    (void)hipGetLastError();
+}
+
 }  // namespace mtx

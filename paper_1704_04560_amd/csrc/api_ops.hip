@@ -512,6 +512,11 @@ int mtx_clip_grads(mtx_clip* c, float max_norm, float* norm_out, void* stream)
     return MTX_OK;
 }
 
-void mtx_free_clip(mtx_clip* c) { delete c; }
+void mtx_free_clip(mtx_clip* c)
+{
+    if (!c) return;
+    finish_stream(c->last_stream);   // its kernels read the caller's workspace
+    delete c;
+}
 
 }  // extern "C"

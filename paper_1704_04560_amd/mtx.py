@@ -431,7 +431,8 @@ def mtx_free_clip(handle):
 
 class Clip:
     """A list of (src, dst) tensors whose global norm is clipped (mtx_clip_grads), with its
-    workspace; keeps the tensors alive."""
+    workspace; keeps the tensors alive.  Closing or dropping it waits for its last call; keep it as
+    long as a graph that holds its calls is replayed."""
 
     def __init__(self, pairs, stream=None):
         import torch
