@@ -285,9 +285,10 @@ int mtx_set_nonfinite_check(mtx_model* m, int enable);
  * applies the update rule, any of mtx_set_optimizer's, from grad_avg.  norm_out (nullable, device
  * fp32 [1]) receives the norm before clipping at every step; workspace is
  * MTX_CLIP_WORKSPACE_BYTES of device scratch, 16-byte aligned; both are the caller's, stay in
- * use until the option is set again, and overlap no model buffer.  The fused and layer-wise
- * updates are not used while it is on.  max_norm = 0 switches it off (the other arguments are
- * then ignored). */
+ * use until the option is set again or the model freed (a call that replaces one of them waits for
+ * the model's last stream; a graph of the caller's that holds a step needs them as long as it is
+ * replayed), and overlap no model buffer.  The fused and layer-wise updates are not used while it is
+ * on.  max_norm = 0 switches it off (the other arguments are then ignored). */
 int mtx_set_clip_norm(mtx_model* m, float max_norm, float* norm_out, void* workspace);
 
 /* Fused average + update of large fully connected layers (execution option, default on).  With

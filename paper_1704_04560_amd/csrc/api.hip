@@ -1181,9 +1181,14 @@ int mtx_set_clip_norm(mtx_model* m, float max_norm, float* norm_out, void* works
         if (norm_out && overlap(norm_out, 4, workspace, MTX_CLIP_WORKSPACE_BYTES))
             return fail(MTX_EINVAL, "norm_out overlaps the workspace");
     }
+    float* const out = max_norm > 0.0f ? norm_out : nullptr;
+    double* const ws = max_norm > 0.0f ? static_cast<double*>(workspace) : nullptr;
+    // steps still running may use buffers that the caller now gets back
+    if ((m->clip_ws && m->clip_ws != ws) || (m->clip_out && m->clip_out != out))
+        finish_stream(m->last_stream);
     m->clip_norm = max_norm;
-    m->clip_out = max_norm > 0.0f ? norm_out : nullptr;
-    m->clip_ws = max_norm > 0.0f ? static_cast<double*>(workspace) : nullptr;
+    m->clip_out = out;
+    m->clip_ws = ws;
     m->graph.reset();  // the captured launch sequence depends on it
     return MTX_OK;
 }

@@ -487,6 +487,7 @@ class Model:
             self.handle = mtx_init_model(self.desc, R, shard_batch, seed, self.w, self.v,
                                          self.grads, self.grad_avg, self.workspace, stream)
         self._shapes = self._out_shapes()
+        self._clip = (None, None)   # norm_out and workspace of set_clip_norm
 
     def _out_shapes(self):
         c, h, w = self.in_shape
@@ -512,13 +513,14 @@ class Model:
 
     def set_clip_norm(self, max_norm, norm_out=None):
         """Clip the averaged gradient's global norm in train_step (0: off); norm_out: a device
-        float32 [1] that receives the norm of every step."""
+        float32 [1] that receives the norm of every step.  A graph that holds a clipped step is
+        replayed only while the option stays on with the same norm_out."""
         import torch
-        ws = None
-        if max_norm > 0:
+        ws = self._clip[1] if max_norm > 0 else None
+        if max_norm > 0 and ws is None:
             ws = torch.empty(MTX_CLIP_WORKSPACE_BYTES, dtype=torch.uint8, device=self.w.device)
         mtx_set_clip_norm(self.handle, max_norm, norm_out, ws)
-        self._clip = (norm_out, ws)
+        self._clip = (norm_out if max_norm > 0 else None, ws)
 
     def set_optimizer(self, kind, beta1=0.9, beta2=0.999, eps=1e-8):
         """Select the update rule of train_step; Adam gets a zeroed second-moment buffer."""

@@ -1,9 +1,11 @@
-"""What a handle or a model gives back to its owner is no longer in use: freeing a clip handle
-waits for the calls that still use its buffers, on whichever stream these run."""
+"""What a handle or a model gives back to its owner is no longer in use: freeing a clip handle or
+changing the clip option's buffers waits for the calls that still use them, on whichever stream
+these run."""
 import pytest
 import torch
 
 from paper_1704_04560_amd import mtx
+from paper_1704_04560_amd import workloads as wl
 
 pytestmark = pytest.mark.gpu
 
@@ -66,3 +68,42 @@ def test_free_inside_a_capture_leaves_it_alone():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, out[:1].expand(N)) and abs(out[0].item() * N ** 0.5 - 1) < 1e-6
+
+
+def _model():
+    net = wl.MLP
+    m = mtx.Model(net.in_shape, wl.layer_tuples(net), net.dtype, 2, 4, seed=1)
+    x, y = (torch.from_numpy(t).cuda() for t in wl.make_batch(net, 8, seed=2))
+    return m, x, y
+
+
+def test_clip_option_waits_for_steps_with_the_old_buffers():
+    m, x, y = _model()
+    nrm = torch.zeros(1, device="cuda")
+    s = torch.cuda.Stream()
+    for last in (dict(max_norm=0), dict(max_norm=0.5, norm_out=torch.zeros(1, device="cuda"))):
+        m.set_clip_norm(0.1, nrm)
+        held = m._clip   # (keeps them while the wait is tested)
+        _busy(s)
+        m.train_step(x, y, 0.01, 0.9, stream=s)
+        assert not s.query()
+        m.set_clip_norm(**last)
+        assert s.query(), last
+        assert held[0].item() > 0.1
+        m.set_clip_norm(0)
+    m.close()
+
+
+def test_another_bound_over_the_same_buffers_does_not_wait():
+    m, x, y = _model()
+    nrm = torch.zeros(1, device="cuda")
+    s = torch.cuda.Stream()
+    m.set_clip_norm(0.1, nrm)
+    _busy(s)
+    m.train_step(x, y, 0.0, 0.0, stream=s)
+    m.set_clip_norm(0.2, nrm)
+    m.train_step(x, y, 0.0, 0.0, stream=s)
+    assert not s.query()
+    torch.cuda.synchronize()
+    assert abs(float(m.grad_avg.double().norm()) - 0.2) <= 1e-6
+    m.close()
