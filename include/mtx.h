@@ -326,6 +326,8 @@ int mtx_set_layerwise_update(mtx_model* m, int enable);
  *         mtx_train_step calls since this call (1 for the first).
  *   AdaGrad: accumulator in the model's v buffer (its content is the initial accumulator;
  *         mtx_set_params sets it); eps >= 0; beta1, beta2 and s2 unused.
+ * A call that replaces s2 waits for the model's last stream; a graph of the caller's that holds a
+ * step needs the old one as long as it is replayed.
  * mtx_get_params / mtx_set_params read and write v as that state.  A step with Adam is never
  * replayed from a graph (its bias correction changes every step).  Returns MTX_EINVAL for an
  * unknown kind, invalid hyperparameters, or an s2 that overlaps the model's buffers. */

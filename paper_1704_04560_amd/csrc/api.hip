@@ -1916,11 +1916,13 @@ int mtx_set_optimizer(mtx_model* m, int kind, float beta1, float beta2, float ep
             (m->clip_out && overlap(s2, nb, m->clip_out, 4)))
             return fail(MTX_EINVAL, "the second-moment buffer overlaps the model's buffers");
     }
+    if (kind != MTX_OPT_ADAM) s2 = nullptr;
+    if (m->s2 && m->s2 != s2) finish_stream(m->last_stream);   // steps still running may use it
     m->opt = kind;
     m->b1 = beta1;
     m->b2 = beta2;
     m->eps = eps;
-    m->s2 = kind == MTX_OPT_ADAM ? s2 : nullptr;
+    m->s2 = s2;
     m->opt_step = 0;
     m->graph.reset();  // a recorded step holds the previous update rule
     return MTX_OK;

@@ -488,6 +488,7 @@ class Model:
                                          self.grads, self.grad_avg, self.workspace, stream)
         self._shapes = self._out_shapes()
         self._clip = (None, None)   # norm_out and workspace of set_clip_norm
+        self.s2 = None              # second moment of set_optimizer
 
     def _out_shapes(self):
         c, h, w = self.in_shape
@@ -525,10 +526,11 @@ class Model:
     def set_optimizer(self, kind, beta1=0.9, beta2=0.999, eps=1e-8):
         """Select the update rule of train_step; Adam gets a zeroed second-moment buffer."""
         import torch
-        self.s2 = None
+        s2 = None
         if kind == MTX_OPT_ADAM:
-            self.s2 = torch.zeros(self.P, dtype=torch.float32, device=self.w.device)
-        mtx_set_optimizer(self.handle, kind, beta1, beta2, eps, self.s2)
+            s2 = torch.zeros(self.P, dtype=torch.float32, device=self.w.device)
+        mtx_set_optimizer(self.handle, kind, beta1, beta2, eps, s2)
+        self.s2 = s2   # (a refused call keeps the present one in use)
 
     def get_params(self):
         w = np.empty(self.P, np.float32)

@@ -1,6 +1,6 @@
-"""What a handle or a model gives back to its owner is no longer in use: freeing a clip handle or
-changing the clip option's buffers waits for the calls that still use them, on whichever stream
-these run."""
+"""What a handle or a model gives back to its owner is no longer in use: freeing a clip handle,
+changing the clip option's buffers or the update rule's state waits for the calls that still use
+them, on whichever stream these run."""
 import pytest
 import torch
 
@@ -106,4 +106,31 @@ def test_another_bound_over_the_same_buffers_does_not_wait():
     assert not s.query()
     torch.cuda.synchronize()
     assert abs(float(m.grad_avg.double().norm()) - 0.2) <= 1e-6
+    m.close()
+
+
+def test_update_rule_waits_for_steps_with_the_old_state():
+    m, x, y = _model()
+    s = torch.cuda.Stream()
+    m.set_optimizer(mtx.MTX_OPT_ADAM)
+    held = m.s2
+    _busy(s)
+    m.train_step(x, y, 0.001, 0.0, stream=s)
+    assert not s.query()
+    m.set_optimizer(mtx.MTX_OPT_MOMENTUM)
+    assert s.query()
+    assert held.any()
+    m.close()
+
+
+def test_a_refused_update_rule_keeps_the_present_state():
+    m, x, y = _model()
+    m.set_optimizer(mtx.MTX_OPT_ADAM)
+    held = m.s2
+    with pytest.raises(mtx.MtxError):
+        m.set_optimizer(mtx.MTX_OPT_ADAM, beta1=2.0)
+    assert m.s2 is held
+    m.train_step(x, y, 0.001, 0.0)
+    torch.cuda.synchronize()
+    assert held.any()
     m.close()
