@@ -396,7 +396,8 @@ void mtx_free_model(mtx_model* m);
  * deterministic run to run: no sum depends on the order in which atomics arrive.  Every call may
  * be captured into a HIP graph.  A workspace is 16-byte aligned device scratch whose content
  * need not survive between calls: calls that overlap in time (other streams, other graphs) need
- * workspaces of their own.  Operand tensors must not overlap unless stated. */
+ * workspaces of their own.  Operand tensors must share no element unless stated; their rows may lie
+ * between one another's (columns of one matrix). */
 
 /* Embedding lookup with scaling:  y[i][:] = scale * w[tokens[i]][:],  i < n, rounded once to
  * y_type; w [V][D] contiguous of w_type, y rows ldy >= D apart.  A token equal to `pad` gives a

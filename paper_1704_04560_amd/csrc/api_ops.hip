@@ -19,28 +19,69 @@ namespace {
 bool known_type(int t) { return t == MTX_F32 || t == MTX_BF16; }
 size_t type_size(int t) { return t == MTX_F32 ? 4 : 2; }
 
-// Byte range [p, p + bytes) of a tensor; bytes = 0 for an absent one.
+// A tensor's bytes: `rows` rows of `bytes` bytes, `stride` apart (at least `bytes`); bytes = 0 for an
+// absent one.
 struct Span {
     const void* p;
     size_t bytes;
     bool written;
+    size_t rows = 1, stride = 0;
 };
 
 Span rows_span(const void* p, long long rows, long long D, long long ld, size_t es, bool written)
 {
-    return Span{p, p && rows > 0 ? (size_t)((rows - 1) * ld + D) * es : 0, written};
+    return Span{p, p && rows > 0 ? (size_t)D * es : 0, written, (size_t)rows, (size_t)ld * es};
+}
+
+// Sum over 0 <= i < n of floor((a i + b) / m) for a, b >= 0 and m > 0: the lattice points under a
+// line.  Whole multiples of m come out of a and b first; the rest is counted by rows (row k holds
+// the i with a i + b >= k m), which is the same sum with a and m exchanged.
+typedef __int128 wide;
+wide points_under_line(wide n, wide a, wide b, wide m)
+{
+    if (n <= 0) return 0;
+    const wide sum = a / m * (n * (n - 1) / 2) + b / m * n;
+    a %= m;
+    b %= m;
+    const wide rows = (a * (n - 1) + b) / m;
+    if (rows == 0) return sum;
+    return sum + rows * n - points_under_line(rows, m, m - b + a - 1, a);
+}
+
+wide floor_div(wide x, wide m) { return x >= 0 ? x / m : -((-x + m - 1) / m); }
+
+// Whether two tensors share a byte; the columns of one matrix may be several tensors.
+bool share_bytes(const Span& a, const Span& b)
+{
+    if (!a.bytes || !b.bytes) return false;
+    if (!overlap(a.p, (a.rows - 1) * a.stride + a.bytes, b.p, (b.rows - 1) * b.stride + b.bytes))
+        return false;
+    if (a.rows == 1 && b.rows == 1) return true;
+    // Row i of a starts x = d + i sa behind b.  It meets the rows j of b with x - lb < j sb < x + la:
+    // floor((x + la - 1) / sb) - floor((x - lb) / sb) of them, of which 0 <= j < b.rows leaves one
+    // at least for the i of i0 .. i1, if it is not empty.
+    const wide la = (wide)a.bytes, lb = (wide)b.bytes;
+    const wide sa = a.rows > 1 ? (wide)a.stride : la, sb = b.rows > 1 ? (wide)b.stride : lb;
+    const wide d = (wide)reinterpret_cast<uintptr_t>(a.p) - (wide)reinterpret_cast<uintptr_t>(b.p);
+    const wide i0 = std::max<wide>(0, -floor_div(la - 1 + d, sa));
+    const wide i1 = std::min<wide>((wide)a.rows - 1,
+                                   floor_div(((wide)b.rows - 1) * sb + lb - 1 - d, sa));
+    // (both floors of a multiple of sb more, so that nothing is negative)
+    const wide x0 = d + i0 * sa + (la + lb + sb) / sb * sb;
+    return points_under_line(i1 - i0 + 1, sa, x0 + la - 1, sb) >
+           points_under_line(i1 - i0 + 1, sa, x0 - lb, sb);
 }
 
 // Whether a written tensor overlaps any other one.
-bool spans_overlap(std::initializer_list<Span> list)
+template <class List> bool spans_overlap(const List& list)
 {
-    for (auto a = list.begin(); a != list.end(); ++a)
-        for (auto b = a + 1; b != list.end(); ++b)
-            if ((a->written || b->written) && a->bytes && b->bytes &&
-                overlap(a->p, a->bytes, b->p, b->bytes))
-                return true;
+    for (auto a = std::begin(list); a != std::end(list); ++a)
+        for (auto b = a + 1; b != std::end(list); ++b)
+            if ((a->written || b->written) && share_bytes(*a, *b)) return true;
     return false;
 }
+
+bool spans_overlap(std::initializer_list<Span> list) { return spans_overlap<>(list); }
 
 constexpr size_t kMaxRows = 2147483647;
 constexpr size_t kMaxTokens = (size_t)1 << 30;
@@ -119,7 +160,7 @@ int mtx_embed_backward(const int32_t* tokens, size_t n, int R, const void* dy, i
     if (workspace_bytes < need)
         return fail(MTX_ENOMEM, "workspace too small: %zu bytes given, %zu needed",
                     workspace_bytes, need);
-    if (spans_overlap({Span{grads, ((R - 1) * ld + vd) * 4, true}, Span{workspace, need, true},
+    if (spans_overlap({rows_span(grads, R, vd, ld, 4, true), Span{workspace, need, true},
                        rows_span(dy, N, D, lddy, es, false), Span{tokens, N * 4, false}}))
         return fail(MTX_EINVAL, "grads, dy, tokens and the workspace must not overlap");
     HIP_TRY(embed_bwd(tokens, (long long)n, R, dy, (Dt)dy_type, (long long)lddy, V, D, pad, scale,
@@ -197,8 +238,7 @@ int mtx_block_norm_forward(const mtx_norm_desc* d, const void* h, const void* x,
     for (const void* p : {h, x, (const void*)h_out, (const void*)y})
         if (!aligned(p, es)) return fail(MTX_EINVAL, "tensors must be aligned to their element size");
     if (!aligned(stats, 16)) return fail(MTX_EINVAL, "stats must be 16-byte aligned");
-    const Span hs = rows_span(h, b.rows, b.D, b.ld_h, es, false);
-    if (spans_overlap({Span{hs.p, h == h_out ? 0 : hs.bytes, false},
+    if (spans_overlap({rows_span(h == h_out ? nullptr : h, b.rows, b.D, b.ld_h, es, false),
                        rows_span(x, b.rows, b.D, b.ld_x, es, false),
                        rows_span(h_out, b.rows, b.D, b.ld_h, es, true),
                        rows_span(y, b.rows, b.D, b.ld_y, es, true),
@@ -262,45 +302,24 @@ int mtx_block_norm_backward(const mtx_norm_desc* d, int R, const void* h_out, co
     if (workspace_bytes < need)
         return fail(MTX_ENOMEM, "workspace too small: %zu bytes given, %zu needed",
                     workspace_bytes, need);
-    // the gradients of several parameters may share rows of one vector [R][ld], each at its own
-    // columns: compared shard by shard where they are strided
-    const float* pg[5] = {d_post_w, d_post_b, d_gate, d_pre_w, d_pre_b};
-    for (int i = 0; i < 5; ++i)
-        for (int j = i + 1; j < 5; ++j) {
-            if (!pg[i] || !pg[j]) continue;
-            if ((i == 2 || j == 2) && b.gate_rows) {
-                const float* o = pg[i == 2 ? j : i];
-                const size_t gb = (size_t)(b.rows / b.gate_rows) * b.D * 4;
-                for (int r = 0; r < R; ++r)
-                    if (overlap(d_gate, gb, o + r * ld, (size_t)b.D * 4))
-                        return fail(MTX_EINVAL, "parameter gradients overlap");
-                continue;
-            }
-            const long long off = (long long)((intptr_t)pg[j] - (intptr_t)pg[i]) / 4;
-            // same stride: rows r of one and r + k of the other collide for some k in (-R, R)
-            const long long dist = off < 0 ? -off : off, q = dist / (long long)ld;
-            const long long lo = dist - q * (long long)ld, hi = (long long)ld - lo;
-            if ((q < R && lo < b.D) || (q + 1 < R && hi < b.D))
-                return fail(MTX_EINVAL, "parameter gradients overlap");
-        }
-    const size_t pb = ((size_t)(R - 1) * ld + b.D) * 4;
-    const size_t gb = b.gate_rows ? (size_t)(b.rows / b.gate_rows) * b.D * 4 : pb;
+    // the gradients of several parameters may share rows of one vector [R][ld], each at its own columns
+    const Span params[] = {rows_span(d_post_w, R, b.D, ld, 4, true), rows_span(d_post_b, R, b.D, ld, 4, true),
+                           b.gate_rows ? rows_span(d_gate, b.rows / b.gate_rows, b.D, b.D, 4, true)
+                                       : rows_span(d_gate, R, b.D, ld, 4, true),
+                           rows_span(d_pre_w, R, b.D, ld, 4, true), rows_span(d_pre_b, R, b.D, ld, 4, true)};
+    if (spans_overlap(params)) return fail(MTX_EINVAL, "parameter gradients overlap");
     const Span in_out[] = {rows_span(h_out, b.rows, b.D, b.ld_h, es, false),
                            rows_span(x, b.rows, b.D, b.ld_x, es, false),
                            rows_span(dy, b.rows, b.D, b.ld_y, es, false),
-                           Span{dh_out, dh_out == dh ? 0 : rows_span(dh_out, b.rows, b.D, b.ld_h, es, false).bytes, false},
+                           rows_span(dh_out == dh ? nullptr : dh_out, b.rows, b.D, b.ld_h, es, false),
                            rows_span(dh, b.rows, b.D, b.ld_h, es, true),
                            rows_span(dx, b.rows, b.D, b.ld_x, es, true),
                            Span{stats, stats ? (size_t)b.rows * 16 : 0, false},
                            Span{workspace, need, true}, NORM_PARAM_SPANS(b)};
-    for (const Span& a : in_out)
-        for (const Span& c : in_out)
-            if (&a != &c && (a.written || c.written) && a.bytes && c.bytes &&
-                overlap(a.p, a.bytes, c.p, c.bytes))
-                return fail(MTX_EINVAL, "an output overlaps another tensor");
-    for (int i = 0; i < 5; ++i)
+    if (spans_overlap(in_out)) return fail(MTX_EINVAL, "an output overlaps another tensor");
+    for (const Span& p : params)
         for (const Span& a : in_out)
-            if (pg[i] && a.bytes && overlap(pg[i], i == 2 ? gb : pb, a.p, a.bytes))
+            if (share_bytes(p, a))
                 return fail(MTX_EINVAL, "a parameter gradient overlaps another tensor");
     const BlockNormGrads g{h_out, want_x ? x : nullptr, stats, dy, dh_out, dh, dx, d_post_w, d_post_b, d_gate,
                            d_pre_w, d_pre_b, (long long)ld, false};
@@ -325,7 +344,7 @@ int mtx_average_clip(const float* grads, int R, size_t n, size_t ld, float max_n
     if (workspace_bytes < MTX_CLIP_WORKSPACE_BYTES)
         return fail(MTX_ENOMEM, "workspace too small: %zu bytes given, %d needed",
                     workspace_bytes, MTX_CLIP_WORKSPACE_BYTES);
-    if (spans_overlap({Span{grads, ((R - 1) * ld + n) * 4, false}, Span{avg, n * 4, true},
+    if (spans_overlap({rows_span(grads, R, n, ld, 4, false), Span{avg, n * 4, true},
                        Span{norm_out, norm_out ? (size_t)4 : 0, true},
                        Span{workspace, MTX_CLIP_WORKSPACE_BYTES, true}}))
         return fail(MTX_EINVAL, "grads, avg, norm_out and the workspace must not overlap");
