@@ -169,6 +169,27 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+_int32 = None   # torch.int32, once torch is there
+
+
+def _ids(t, name: str) -> Optional[int]:
+    """Address of tokens or labels, which the library reads as int32 one after the other (torch's own
+    integers are int64, and a sequence without its last token is not contiguous)."""
+    global _int32
+    if t is None or isinstance(t, int):
+        return t
+    if isinstance(t, np.ndarray):
+        ok = t.dtype == np.int32 and t.flags.c_contiguous
+    else:
+        if _int32 is None:
+            import torch
+            _int32 = torch.int32
+        ok = t.dtype is _int32 and t.is_contiguous()
+    if not ok:
+        raise ValueError(f"{name} must be contiguous int32")
+    return _ptr(t)
+
+
 _raw_stream = None   # (): the current stream's handle
 
 
@@ -224,13 +245,13 @@ def mtx_init_model_static(desc, R, shard_batch, seed, w, v, grads, grad_avg, str
 
 
 def mtx_train_step(handle, x, labels, lr, momentum, loss_out=None, stream=None):
-    _check(lib().mtx_train_step(handle, _ptr(x), _ptr(labels), lr, momentum, _ptr(loss_out),
-                                _stream(stream)))
+    _check(lib().mtx_train_step(handle, _ptr(x), _ids(labels, "labels"), lr, momentum,
+                                _ptr(loss_out), _stream(stream)))
 
 
 def mtx_train_step_tokens(handle, tokens, labels, lr, momentum, loss_out=None, stream=None):
-    _check(lib().mtx_train_step_tokens(handle, _ptr(tokens), _ptr(labels), lr, momentum,
-                                       _ptr(loss_out), _stream(stream)))
+    _check(lib().mtx_train_step_tokens(handle, _ids(tokens, "tokens"), _ids(labels, "labels"), lr,
+                                       momentum, _ptr(loss_out), _stream(stream)))
 
 
 def mtx_set_embedding(handle, scale=1.0, pad=-1):
@@ -338,8 +359,8 @@ def _bytes(t) -> int:
 
 
 def mtx_embed_forward(w, w_type, V, D, tokens, n, pad, scale, y, y_type, ldy, stream=None):
-    _check(lib().mtx_embed_forward(_ptr(w), w_type, V, D, _ptr(tokens), n, pad, scale, _ptr(y),
-                                   y_type, ldy, _stream(stream)))
+    _check(lib().mtx_embed_forward(_ptr(w), w_type, V, D, _ids(tokens, "tokens"), n, pad, scale,
+                                   _ptr(y), y_type, ldy, _stream(stream)))
 
 
 def mtx_embed_sizes(n, R, V, D) -> int:
@@ -350,8 +371,8 @@ def mtx_embed_sizes(n, R, V, D) -> int:
 
 def mtx_embed_backward(tokens, n, R, dy, dy_type, lddy, V, D, pad, scale, grads, ld, accumulate,
                        workspace, stream=None):
-    _check(lib().mtx_embed_backward(_ptr(tokens), n, R, _ptr(dy), dy_type, lddy, V, D, pad, scale,
-                                    _ptr(grads), ld, 1 if accumulate else 0, _ptr(workspace),
+    _check(lib().mtx_embed_backward(_ids(tokens, "tokens"), n, R, _ptr(dy), dy_type, lddy, V, D, pad,
+                                    scale, _ptr(grads), ld, 1 if accumulate else 0, _ptr(workspace),
                                     _bytes(workspace), _stream(stream)))
 
 
