@@ -321,6 +321,7 @@ struct EmbedGather {
     long long lddy;
     int n, R, V, D, lg, bins;
     int P, BP, pieces, slices; // positions of a group, of a block; blocks along a shard; along D
+    long long piece0;          // the launch's first piece of all shards'
     float scale;
     float* grads;
     long long ld;
@@ -394,7 +395,7 @@ __global__ __launch_bounds__(kGroups * L) void embed_gather_kernel(EmbedGather a
     __shared__ int edge_row[G][2];   // their rows, -1: none
     __shared__ int head_ends[G];     // the head's row ends in the group
     const int slice = (int)(blockIdx.x % a.slices);
-    const long long pc = blockIdx.x / a.slices;
+    const long long pc = a.piece0 + blockIdx.x / a.slices;
     const int r = (int)(pc / a.pieces), p = (int)(pc % a.pieces);
     const int nv = a.valid[r];
     const int b0 = p * G * a.P;
@@ -658,8 +659,12 @@ static hipError_t launch_gather(EmbedGather a, hipStream_t s)
     a.BP = G * a.P;
     a.pieces = (a.n + a.BP - 1) / a.BP;
     const long long pieces = (long long)a.R * a.pieces;
-    hipLaunchKernelGGL((embed_gather_kernel<T, E, VEC, L>), dim3((unsigned)(pieces * a.slices)),
-                       dim3(kGroups * L), 0, s, a);
+    // (a launch has fewer than 2^32 threads: many shards of few tokens and wide rows take several)
+    const long long most = std::max(1LL, ((1LL << 32) / (kGroups * L) - 1) / a.slices);
+    for (a.piece0 = 0; a.piece0 < pieces; a.piece0 += most)
+        hipLaunchKernelGGL((embed_gather_kernel<T, E, VEC, L>),
+                           dim3((unsigned)(std::min(most, pieces - a.piece0) * a.slices)),
+                           dim3(kGroups * L), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.pieces <= 1) return e;
     timing_split(s, "join");
