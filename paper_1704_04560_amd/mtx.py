@@ -460,6 +460,8 @@ class Clip:
         self.handle = None
         self.pairs = list(pairs)
         tensors = make_tensor_list(self.pairs)
+        if any(not src.is_cuda or src.device != self.pairs[0][0].device for src, _ in self.pairs):
+            raise ValueError("the tensors must be on one GPU")
         self.workspace = torch.empty(mtx_clip_sizes(tensors), dtype=torch.uint8,
                                      device=self.pairs[0][0].device)
         self.handle = mtx_init_clip(tensors, self.workspace, stream)
