@@ -445,6 +445,8 @@ int mtx_init_clip(const mtx_tensor* tensors, int count, void* workspace, size_t 
         if (workspace_bytes < need)
             return fail(MTX_ENOMEM, "workspace too small: %zu bytes given, %zu needed",
                         workspace_bytes, need);
+        if (being_captured(static_cast<hipStream_t>(stream)))
+            return fail(MTX_EINVAL, "the stream is being captured: make the handle before");
         std::vector<ClipChunk> table;
         table.reserve(chunks);
         bool in_place = true;

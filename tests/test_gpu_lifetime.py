@@ -134,3 +134,24 @@ def test_a_refused_update_rule_keeps_the_present_state():
     torch.cuda.synchronize()
     assert held.any()
     m.close()
+
+
+def test_a_handle_made_inside_a_capture_is_refused():
+    """... and the capture goes on."""
+    a, out = _grad(), torch.zeros(N, device="cuda")
+    other = _grad()
+    b = mtx.make_tensor_list([(other, None)])
+    ws = torch.empty(mtx.mtx_clip_sizes(b), dtype=torch.uint8, device="cuda")
+    clip = mtx.Clip([(a, out)])
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        with pytest.raises(mtx.MtxError) as e:
+            mtx.mtx_init_clip(b, ws)
+        clip.clip(1.0)
+    assert e.value.code == mtx.MTX_EINVAL
+    for k in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, out[:1].expand(N)) and abs(out[0].item() * N ** 0.5 - 1) < 1e-6
