@@ -41,10 +41,14 @@ inline bool being_captured(hipStream_t s)
 }
 
 // Wait for what was enqueued on a stream.  Calls on a stream that is being captured have not run,
-// and waiting for them would end the capture.
+// and waiting for them would end the capture; so would waiting for any other stream while one is
+// captured, unless the thread's calls are declared apart from captures (relaxed).
 inline void finish_stream(hipStream_t s)
 {
+    hipStreamCaptureMode mode = hipStreamCaptureModeRelaxed;
+    const bool relaxed = hipThreadExchangeStreamCaptureMode(&mode) == hipSuccess;
     if (!being_captured(s)) (void)hipStreamSynchronize(s);
+    if (relaxed) (void)hipThreadExchangeStreamCaptureMode(&mode);
     (void)hipGetLastError();
 }
 

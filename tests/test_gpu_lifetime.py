@@ -155,3 +155,31 @@ def test_a_handle_made_inside_a_capture_is_refused():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, out[:1].expand(N)) and abs(out[0].item() * N ** 0.5 - 1) < 1e-6
+
+
+@pytest.mark.parametrize("own_stream", [False, True])
+@pytest.mark.parametrize("busy", [False, True])
+def test_a_clip_dropped_while_another_stream_is_captured(own_stream, busy):
+    """... waits for its own call and leaves the capture alone."""
+    a, out = _grad(), torch.zeros(N, device="cuda")
+    b, out_b = _grad(), torch.zeros(N, device="cuda")
+    clip, other = mtx.Clip([(a, out)]), mtx.Clip([(b, out_b)])
+    s = torch.cuda.Stream() if own_stream else torch.cuda.default_stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    if not busy:
+        other.clip(1.0, stream=s)
+    with torch.cuda.graph(graph):
+        clip.clip(1.0)
+        if busy:
+            with torch.cuda.stream(s):
+                torch.cuda._sleep(200_000_000)
+            other.clip(1.0, stream=s)
+        del other
+    assert s.query()
+    for k in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for t in (out, out_b):
+            assert torch.equal(t, t[:1].expand(N)) and abs(t[0].item() * N ** 0.5 - 1) < 1e-6
