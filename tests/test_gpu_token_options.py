@@ -115,3 +115,43 @@ def test_projections_from_an_embedding_and_a_norm(R, Nb):
             assert max(rel) <= parity.TOL[wl.F32], (i, r, rel)
             at += size
     m.close()
+
+
+@pytest.mark.parametrize("dtype", [wl.F32, wl.BF16])
+def test_stored_outputs_of_the_token_layers(dtype):
+    """The embedding's rows bit for bit, and each norm from the stored outputs before it: fp32 sums of
+    24 terms and a dozen operations around them, and the rounding of what is stored."""
+    C, T, R, Nb = 24, 10, 2, 3
+    net = wl.Net("outputs", (1, 5, 2), (wl.embed(50, C), wl.norm(), wl.conv(C, 1), wl.norm(False),
+                                        wl.add(0), wl.norm(), wl.fc(3)), dtype, "normal")
+    m = tokens._model(net, R, Nb, seed=6)
+    mtx.mtx_set_embedding(m.handle, 5.0, 7)
+    tokens._spread(m, 2)
+    w = m.get_params()[0]
+    tok, lab = tokens._batch(net, R * Nb, 4)
+    tok[0, 3] = 7
+    m.train_step(tok.cuda(), lab.cuda(), 0.01, 0.9)
+    out = [torch.from_numpy(m.layer_output(i)).view(R * Nb, -1, T) for i in range(6)]
+    table = torch.from_numpy(w[:50 * C]).view(50, C)
+    rows = table[tok.long()] * 5.0
+    rows[tok == 7] = 0.0
+    want = (rows.bfloat16().float() if dtype == wl.BF16 else rows).transpose(1, 2)
+    assert torch.equal(out[0], want)
+    step = 2.0 ** -8 if dtype == wl.BF16 else 0.0
+    total = out[0].double() + out[3].double()
+    assert ((out[4].double() - total).abs() <= (step + 2.0 ** -24) * total.abs()).all()
+    where = np.cumsum([0] + tokens._param_sizes(net))
+    for i, src, p, layer in ((1, out[0].double(), 1, True), (3, out[2].double(), 5, False),
+                             (5, total, 6, True)):
+        a = src - src.mean(1, keepdim=True) if layer else src
+        r = 1 / torch.sqrt(a.square().mean(1, keepdim=True) + 1e-5)
+        g = torch.from_numpy(w[where[p]:where[p] + C]).double()[:, None]
+        y = a * r * g
+        if layer:
+            y = y + torch.from_numpy(w[where[p + 1]:where[p + 1] + C]).double()[:, None]
+        # fp32: sums of 24 terms and a dozen operations on values of the row's size
+        scale = (src.abs() + src.abs().mean(1, keepdim=True)) * r * g.abs() + y.abs()
+        cond = src.square().mean(1, keepdim=True) * r * r
+        tol = step * y.abs() + 64 * 2.0 ** -24 * scale * (1 + cond)
+        assert ((out[i].double() - y).abs() <= tol).all(), i
+    m.close()
