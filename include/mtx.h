@@ -416,7 +416,8 @@ int mtx_embed_sizes(size_t n, int R, int V, int D, size_t* workspace_bytes);
  * without a token are then neither read nor written).  Padding tokens and tokens outside [0, V)
  * contribute nothing (their rows of dy are not read).  tokens [R*n]; dy [R*n] rows of dy_type,
  * lddy >= D apart; ld >= V*D; R <= 65536, R*V <= 2^28, R*n <= 2^30, R*n*D <= 2^36.  The tokens are
- * sorted, and each row's terms added in a fixed order. */
+ * sorted, and each row's terms added in a fixed order.  The sort reads a shard's tokens once or twice
+ * for every 512 rows of the table: its time grows with the product of both. */
 int mtx_embed_backward(const int32_t* tokens, size_t n, int R, const void* dy, int dy_type,
                        size_t lddy, int V, int D, int pad, float scale, float* grads, size_t ld,
                        int accumulate, void* workspace, size_t workspace_bytes, void* stream);
