@@ -58,6 +58,40 @@ def test_block_norm_over_columns(N, D, gap, dtype):
     assert torch.equal(A[:, 4 * D:], tail[0]) and torch.equal(G[:, 4 * D:], tail[1])
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,D,group", [(9, 8, 3), (130, 64, 0), (64, 120, 4), (1100, 256, 1), (33, 1000, 0),
+                                       (12, 4096, 2)])
+def test_strides_of_their_own(N, D, group, dtype):
+    """The stream, the block's output and the norm with three strides: the bits of packed rows."""
+    print(f"[case] strides N={N} D={D} group={group} {dtype}", flush=True)
+    g = _gen(N * D)
+    p = _params(g, D)
+    p["gate"] = torch.randn(N // group if group else 1, D, generator=g).cuda()
+    t = [torch.randn(N, D, generator=g).to(dtype).cuda() for _ in range(4)]   # h, x, dy, dh_out
+    res = []
+    for lh, lx, ly in ((D + 8, 2 * D + 40, D + 24), (D, D, D)):
+        def rows(ld, src=None):
+            m = torch.full((N, ld), 3.0, dtype=dtype, device="cuda")
+            if src is not None:
+                m[:, :D] = src
+            return m
+
+        d = mtx.make_norm_desc(mtx.MTX_NORM_LAYER, MT[dtype], N, D, 1e-5, 0.5, group, p["post_w"],
+                               p["post_b"], p["gate"], p["pre_w"], p["pre_b"], lh, lx, ly)
+        h, x, H, y = rows(lh, t[0]), rows(lx, t[1]), rows(lh), rows(ly)
+        dy, dho, dh, dx = rows(ly, t[2]), rows(lh, t[3]), rows(lh), rows(lx)
+        st, gr, gg = (torch.empty(N, 4, device="cuda"), torch.empty(5, D, device="cuda"),
+                      torch.empty_like(p["gate"]))
+        ws = torch.empty(mtx.mtx_block_norm_sizes(d, 1), dtype=torch.uint8, device="cuda")
+        mtx.mtx_block_norm_forward(d, h, x, H, y, st)
+        mtx.mtx_block_norm_backward(d, 1, H, x, st, dy, dho, dh, dx, gr[0], gr[1], gg, gr[3], gr[4], D, ws)
+        torch.cuda.synchronize()
+        assert all((m[:, D:] == 3.0).all() for m in (h, x, H, y, dy, dho, dh, dx))
+        res.append([m[:, :D].clone() for m in (H, y, dh, dx)] + [st, gr[[0, 1, 3, 4]], gg])
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+
+
 def test_every_placement_of_rows():
     """Random places and strides in one small buffer, against a comparison of every element."""
     rng = random.Random(5)
