@@ -394,9 +394,9 @@ void mtx_free_model(mtx_model* m);
  * elements; pointers are aligned to their element size at least (16-byte aligned rows are read
  * faster).  Sums, statistics and parameter gradients are fp32 or wider.  Results are
  * deterministic run to run: no sum depends on the order in which atomics arrive.  Every call but
- * mtx_init_clip may be captured into a HIP graph.  A workspace is 16-byte aligned device scratch whose content
- * need not survive between calls: calls that overlap in time (other streams, other graphs) need
- * workspaces of their own.  Operand tensors must share no element unless stated; their rows may lie
+ * mtx_init_clip may be captured into a HIP graph.  A workspace is 16-byte aligned device scratch
+ * whose content need not survive between calls: calls that overlap in time (other streams, other
+ * graphs) need workspaces of their own.  Operand tensors must share no element unless stated; their rows may lie
  * between one another's (columns of one matrix). */
 
 /* Embedding lookup with scaling:  y[i][:] = scale * w[tokens[i]][:],  i < n, rounded once to
@@ -490,12 +490,12 @@ int mtx_average_clip(const float* grads, int R, size_t n, size_t ld, float max_n
 /* The same over a list of tensors of either type.  Each is `n` contiguous elements at src (n may
  * be 0); dst receives the clipped elements, rounded to dst_type: dst = src (same type) clips in
  * place, dst = NULL only counts towards the norm.  No dst may overlap another tensor's src or
- * dst, nor norm_out any of them.  The handle keeps the list in the caller's workspace (mtx_clip_sizes bytes, 256-byte
- * aligned), which with the tensors must stay valid until mtx_free_clip; mtx_init_clip copies it
- * there and synchronises with `stream`, which must not be being captured.  A handle must not be used on two streams at once.
- * mtx_free_clip waits for the stream of the handle's last call, which must still exist (it does not
- * wait for one that is being captured); a graph that holds calls of the handle needs the workspace
- * and the tensors for as long as it is replayed. */
+ * dst, nor norm_out any of them.  The handle keeps the list in the caller's workspace
+ * (mtx_clip_sizes bytes, 256-byte aligned), which with the tensors must stay valid until
+ * mtx_free_clip; mtx_init_clip copies it there and synchronises with `stream`, which must not be
+ * being captured.  A handle must not be used on two streams at once.  mtx_free_clip waits for the
+ * stream of the handle's last call that was not captured, which must still exist; a graph that holds
+ * calls of the handle needs the workspace and the tensors for as long as it is replayed. */
 typedef struct {
     const void* src;
     void* dst;

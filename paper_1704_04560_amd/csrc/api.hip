@@ -831,6 +831,7 @@ struct mtx_model {
     float* gavg;
     char* ws;
     hipStream_t last_stream;
+    hipStream_t eager_stream;   // of the last step that was not captured by the caller
     Timer timer;
     GraphCache graph;
     // second stream for the weight gradients (overlapped with the data-gradient chain), third
@@ -1063,7 +1064,7 @@ static int init_model(const mtx_model_desc* desc, int R, int shard_batch, uint64
     m->w = bufs->w; m->v = bufs->v; m->grads = bufs->grads; m->gavg = bufs->grad_avg;
     m->ws = static_cast<char*>(wsp);
     m->static_ws = static_ws != nullptr;
-    m->last_stream = static_cast<hipStream_t>(stream);
+    m->last_stream = m->eager_stream = static_cast<hipStream_t>(stream);
     // Measured on MI355X: running the weight gradients beside the data-gradient chain gains a
     // few percent when the step's matrix work is large (CIFAR-, AlexNet-sized steps) and loses
     // on small steps, whose kernels each fill the GPU on their own (LeNet).
@@ -1100,6 +1101,23 @@ static int init_model(const mtx_model_desc* desc, int R, int shard_batch, uint64
     return MTX_OK;
 }
 
+// The model's steps: a step that the caller captures leaves the ones before it running.
+static hipError_t sync_model(const mtx_model* m)
+{
+    if (m->eager_stream != m->last_stream) {
+        const hipError_t e = hipStreamSynchronize(m->eager_stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipStreamSynchronize(m->last_stream);
+}
+
+// The same before buffers are given up, also inside a capture.
+static void finish_model(const mtx_model* m)
+{
+    if (m->eager_stream != m->last_stream) finish_stream(m->eager_stream);
+    finish_stream(m->last_stream);
+}
+
 extern "C" {
 
 int mtx_init_model(const mtx_model_desc* desc, int R, int shard_batch, uint64_t seed,
@@ -1124,9 +1142,9 @@ int mtx_init_model_static(const mtx_model_desc* desc, int R, int shard_batch, ui
 void mtx_free_model(mtx_model* m)
 {
     if (!m) return;
-    (void)hipStreamSynchronize(m->last_stream);
-    if (m->side) (void)hipStreamSynchronize(m->side);
-    if (m->upd) (void)hipStreamSynchronize(m->upd);
+    finish_model(m);
+    if (m->side) finish_stream(m->side);
+    if (m->upd) finish_stream(m->upd);
     m->graph.destroy();
     m->timer.destroy();
     destroy_streams(m);
@@ -1185,7 +1203,7 @@ int mtx_set_clip_norm(mtx_model* m, float max_norm, float* norm_out, void* works
     double* const ws = max_norm > 0.0f ? static_cast<double*>(workspace) : nullptr;
     // steps still running may use buffers that the caller now gets back
     if ((m->clip_ws && m->clip_ws != ws) || (m->clip_out && m->clip_out != out))
-        finish_stream(m->last_stream);
+        finish_model(m);
     m->clip_norm = max_norm;
     m->clip_out = out;
     m->clip_ws = ws;
@@ -1837,6 +1855,7 @@ static int train_step(mtx_model* m, const float* x, bool tokens, const int32_t* 
         return fail(MTX_EUNSUPPORTED, "the non-finite check needs the momentum rule and a stream "
                                       "that is not being captured");
     m->last_stream = s;
+    if (!caller_capturing) m->eager_stream = s;
     ++m->opt_step;
     if (m->check_finite) {
         const int rc = step_dispatch(m, x, labels, lr, momentum, loss_out, s, caller_capturing);
@@ -1917,7 +1936,7 @@ int mtx_set_optimizer(mtx_model* m, int kind, float beta1, float beta2, float ep
             return fail(MTX_EINVAL, "the second-moment buffer overlaps the model's buffers");
     }
     if (kind != MTX_OPT_ADAM) s2 = nullptr;
-    if (m->s2 && m->s2 != s2) finish_stream(m->last_stream);   // steps still running may use it
+    if (m->s2 && m->s2 != s2) finish_model(m);   // steps still running may use it
     m->opt = kind;
     m->b1 = beta1;
     m->b2 = beta2;
@@ -2058,7 +2077,7 @@ int mtx_adagrad_update(float* w, float* acc, const float* grads, int R, size_t n
 int mtx_get_params(const mtx_model* m, float* w_host, float* v_host)
 {
     if (!m || !w_host) return fail(MTX_EINVAL, "model and w_host must not be NULL");
-    HIP_TRY(hipStreamSynchronize(m->last_stream), "synchronise");
+    HIP_TRY(sync_model(m), "synchronise");
     HIP_TRY(hipMemcpy(w_host, m->w, m->pl.P * 4, hipMemcpyDeviceToHost), "copy w");
     if (v_host) HIP_TRY(hipMemcpy(v_host, m->v, m->pl.P * 4, hipMemcpyDeviceToHost), "copy v");
     return MTX_OK;
@@ -2067,7 +2086,7 @@ int mtx_get_params(const mtx_model* m, float* w_host, float* v_host)
 int mtx_set_params(mtx_model* m, const float* w_host, const float* v_host)
 {
     if (!m || !w_host) return fail(MTX_EINVAL, "model and w_host must not be NULL");
-    HIP_TRY(hipStreamSynchronize(m->last_stream), "synchronise");
+    HIP_TRY(sync_model(m), "synchronise");
     HIP_TRY(hipMemcpy(m->w, w_host, m->pl.P * 4, hipMemcpyHostToDevice), "copy w");
     if (v_host) HIP_TRY(hipMemcpy(m->v, v_host, m->pl.P * 4, hipMemcpyHostToDevice), "copy v");
     return MTX_OK;
@@ -2082,7 +2101,7 @@ int mtx_get_layer_output(const mtx_model* m, int layer, float* dst_host, size_t 
     const LayerPlan& lp = m->pl.L[layer];
     const size_t cnt = lp.out_elems * m->pl.B;
     if (n < cnt) return fail(MTX_EINVAL, "dst_host holds %zu elements, %zu needed", n, cnt);
-    HIP_TRY(hipStreamSynchronize(m->last_stream), "synchronise");
+    HIP_TRY(sync_model(m), "synchronise");
     std::vector<float> dev;
     std::vector<uint16_t> tmp;
     try {
@@ -2121,7 +2140,7 @@ int mtx_get_pool_argmax(const mtx_model* m, int layer, uint8_t* dst_host, size_t
     const LayerPlan& lp = m->pl.L[layer];
     const size_t cnt = lp.out_elems * m->pl.B;
     if (n < cnt) return fail(MTX_EINVAL, "dst_host holds %zu elements, %zu needed", n, cnt);
-    HIP_TRY(hipStreamSynchronize(m->last_stream), "synchronise");
+    HIP_TRY(sync_model(m), "synchronise");
     std::vector<uint8_t> dev;
     try {
         dev.resize(cnt);

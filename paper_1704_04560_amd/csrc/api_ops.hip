@@ -362,7 +362,7 @@ struct mtx_clip {
     bool in_place;   // every dst is its src or NULL: nothing to write where nothing is clipped
     double* part;
     ClipChunk* table;
-    hipStream_t last_stream;
+    hipStream_t last_stream;   // of the last call that was not captured
 };
 
 // Chunks of a list: pieces of at most kClipChunk elements.
@@ -527,9 +527,10 @@ int mtx_clip_grads(mtx_clip* c, float max_norm, float* norm_out, void* stream)
         if (it != c->spans.begin() && (--it)->second > a)
             return fail(MTX_EINVAL, "norm_out overlaps a tensor of the list or the workspace");
     }
-    c->last_stream = static_cast<hipStream_t>(stream);
-    HIP_TRY(clip_list(c->table, c->chunks, c->in_place, max_norm, norm_out, c->part,
-                      c->last_stream), "mtx_clip_grads");
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (s != c->last_stream && !being_captured(s)) c->last_stream = s;
+    HIP_TRY(clip_list(c->table, c->chunks, c->in_place, max_norm, norm_out, c->part, s),
+            "mtx_clip_grads");
     return MTX_OK;
 }
 

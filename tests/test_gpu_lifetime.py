@@ -183,3 +183,47 @@ def test_a_clip_dropped_while_another_stream_is_captured(own_stream, busy):
         torch.cuda.synchronize()
         for t in (out, out_b):
             assert torch.equal(t, t[:1].expand(N)) and abs(t[0].item() * N ** 0.5 - 1) < 1e-6
+
+
+def test_a_captured_call_does_not_hide_an_earlier_one():
+    """Work on one stream, then a call captured on another: the free waits for the work."""
+    a, out = _grad(), torch.zeros(N, device="cuda")
+    tensors = mtx.make_tensor_list([(a, out)])
+    ws = torch.empty(mtx.mtx_clip_sizes(tensors), dtype=torch.uint8, device="cuda")
+    handle = mtx.mtx_init_clip(tensors, ws)
+    s = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(200_000_000)
+        mtx.mtx_clip_grads(handle, 1.0, stream=s)
+        mtx.mtx_clip_grads(handle, 1.0)
+    mtx.mtx_free_clip(handle)
+    assert s.query()
+    assert torch.equal(out, out[:1].expand(N)) and abs(out[0].item() * N ** 0.5 - 1) < 1e-6
+
+
+@pytest.mark.parametrize("what", ["clip", "rule", "free"])
+def test_a_captured_step_does_not_hide_an_earlier_one(what):
+    m, x, y = _model()
+    m.set_optimizer(mtx.MTX_OPT_ADAM)
+    m.set_clip_norm(1.0)
+    held = m._clip, m.s2, m.w, m.v, m.grads, m.grad_avg, m.workspace
+    s = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(200_000_000)
+        m.train_step(x, y, 0.01, 0.9, stream=s)
+        m.train_step(x, y, 0.01, 0.9)
+    if what == "clip":
+        m.set_clip_norm(0)
+    elif what == "rule":
+        m.set_optimizer(mtx.MTX_OPT_MOMENTUM)
+    else:
+        m.close()
+    assert s.query()
+    del graph, held
+    m.close()
