@@ -227,3 +227,24 @@ def test_a_captured_step_does_not_hide_an_earlier_one(what):
     assert s.query()
     del graph, held
     m.close()
+
+
+@pytest.mark.parametrize("overlap", [False, True])
+def test_a_model_closed_while_another_stream_is_captured(overlap):
+    m, x, y = _model()
+    n, _, _ = _model()
+    want, _, _ = _model()
+    mtx.mtx_set_overlap(n.handle, overlap)
+    n.train_step(x, y, 0.01, 0.9)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        m.train_step(x, y, 0.01, 0.9)
+        n.close()
+    for k in range(3):
+        graph.replay()
+        want.train_step(x, y, 0.01, 0.9)
+        torch.cuda.synchronize()
+        assert torch.equal(m.w, want.w) and torch.equal(m.v, want.v), k
+    m.close()
+    want.close()
