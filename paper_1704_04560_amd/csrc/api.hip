@@ -1222,7 +1222,7 @@ int mtx_set_fused_update(mtx_model* m, int enable)
 int mtx_set_layerwise_update(mtx_model* m, int enable)
 {
     if (!m) return fail(MTX_EINVAL, "model is NULL");
-    // the third stream exists only while it is used: the box exposes few hardware queues, and
+    // the third stream exists only while it is used: a process has few hardware queues, and
     // an idle extra stream can leave the weight-gradient stream sharing one with the caller's
     if (enable && !m->upd) {
         hipError_t e = hipStreamCreateWithFlags(&m->upd, hipStreamNonBlocking);
